@@ -22,3 +22,5 @@ from .binding import (  # noqa: F401
     taper_probe_result,
     TAPER_OK, TAPER_EINVAL, TAPER_EBLOCK, TAPER_EGROUP, TAPER_ELEN, TAPER_EHIP, TAPER_ENOMEM,
 )
+from .latent import LATENT_EXPORTED, LatentContext, LatentPlan  # noqa: F401
+from .pages import PAGES_EXPORTED, PageMover, PagePool, remap_pages  # noqa: F401

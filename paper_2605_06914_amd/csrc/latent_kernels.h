@@ -1,0 +1,68 @@
+// Interface between the host code of the latent-cache operators and their kernels (device pointers only).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "taper_latent.h"
+
+namespace taper {
+
+constexpr int kLatentTileTokens = 64;  // tokens a workgroup of the decode kernel takes at a time: a page per wave
+constexpr int kLatentTileRows = 64;    // query rows it holds at most
+constexpr int kRopeDim = 64;
+
+struct LatentShape {
+    int n_heads, latent_dim, head_dim;
+    float scale_log2e;  // scale * log2(e)
+};
+
+struct LatentDecodeArgs {
+    const int32_t* bt;              // [n_seqs][bt_stride]
+    const taper_latent_item* items;
+    const int32_t* piece_start;     // [n_seqs + 1]
+    const int32_t* piece_row;
+    void* q_lat;                    // bf16 [n_seqs * n_heads][latent_dim + 64]
+    float2* ml;                     // [n_partial_rows] running max in log2 units, sum
+    void* part;                     // [n_partial_rows][latent_dim] rows divided by their own sum
+    const void* q;
+    const void* w_up;
+    const void* pages;
+    void* out;
+    float* lse;
+    int32_t bt_stride, n_seqs, n_items, row_tiles;  // row_tiles: the widest item's, in 16 rows
+};
+hipError_t launch_latent_decode(const LatentShape& sh, const LatentDecodeArgs& a, hipStream_t s);
+
+// A tile of a prompt's query rows.
+struct PromptTile {
+    int32_t row0, n_rows;        // rows of q
+    int32_t first_pos;           // position of the first row's token in its sequence
+    int32_t prefix_len;          // tokens of the shared prefix
+    int32_t prefix_e, suffix_e;  // expanded pages of the prefix and of the private tokens begin here
+    int32_t page_begin, page_end;  // the pages of the sequence (prefix pages, then private ones) this tile's item meets
+    int32_t part_row;            // partial rows of head 0, or -1: the item is its rows' only one and writes the result
+    int32_t n_pieces;            // items of the same rows; their partial rows are n_rows apart
+};
+struct PromptArgs {
+    const int32_t* e_page;       // [n_expanded] physical page of an expanded page
+    const int32_t* e_valid;      // [n_expanded] tokens of it that exist
+    const PromptTile* tiles;     // [n_tiles], longest first
+    const PromptTile* merges;    // [n_merges] row tiles whose keys are cut into pieces
+    void* kv;                    // bf16 [head of the group][n_expanded][K | V], tiles as in the pool of taper_attn.h
+    float2* ml;
+    float* part;                 // [head][partial rows][head_dim]
+    const void* q;
+    const void* w_up;
+    const void* pages;
+    void* out;
+    float* lse;
+    int32_t n_expanded, n_tiles, n_merges, n_partial_rows;  // partial rows of one head
+    int32_t heads_at_once;
+};
+hipError_t launch_latent_prompt(const LatentShape& sh, const PromptArgs& a, hipStream_t s);
+
+hipError_t launch_latent_append(int latent_dim, int64_t n, const void* latent, int64_t latent_stride, const void* rope, int64_t rope_stride,
+                                const int64_t* slots, void* pages, int64_t n_slots, hipStream_t s);
+
+}  // namespace taper

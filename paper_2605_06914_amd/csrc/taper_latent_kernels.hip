@@ -1,0 +1,331 @@
+// gfx950 kernels of the decode step over a latent cache: one vector c_t of R values and a rotated key part r_t of 64 values
+// a token, read once for all heads.
+//
+// Three launches.  absorb_kernel rewrites the queries, q_lat = (W_k[h]^T q_n, q_r).  latent_decode_kernel computes
+// softmax(scale q_lat . (c, r)) . c for items of up to 64 query rows and some tokens, as partial rows.  finish_kernel merges
+// a row's partials through their (max, sum) and applies W_v[h].
+#include <cmath>
+
+#include "latent_device.h"
+
+namespace taper {
+namespace latent {
+
+// ---------------------------------------------------------------------------
+// absorb: q_lat[s,h,r] = sum_n q[s,h,n] W_k[h][n][r].  The contraction runs over W's rows, so a matrix operand needs 8 rows of
+// one column in a lane: a lane loads 16 bytes of each of 8 rows and transposes the 8 x 8 block in registers (a v_perm per
+// register).  Its 8 columns go to 8 different products, whose results then hold 8 consecutive r of a query.  One wave a
+// (head, 128 columns); W is read once and stays in registers for all sequences.
+// ---------------------------------------------------------------------------
+template <int KS>  // head_dim / 32
+__global__ __launch_bounds__(64) void absorb_kernel(const LatentShape sh, const LatentDecodeArgs a, const int s_per_block) {
+    const int lane = threadIdx.x, n = lane & 15, g = lane >> 4, h = blockIdx.x, r0 = blockIdx.y * 128;
+    const int R = sh.latent_dim, KD = R + kRopeDim, HD = 32 * KS, H = sh.n_heads;
+    const __bf16* w = (const __bf16*)a.w_up + (int64_t)h * 2 * HD * R + r0 + 8 * n;
+    bf16x8 wf[KS][8];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        u32x4 row[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) row[j] = *(const u32x4*)(w + (int64_t)(32 * ks + 8 * g + j) * R);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            u32x4 c;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                c[j] = __builtin_amdgcn_perm(row[2 * j + 1][i / 2], row[2 * j][i / 2], i & 1 ? 0x07060302u : 0x05040100u);
+            wf[ks][i] = __builtin_bit_cast(bf16x8, c);
+        }
+    }
+    const int s_end = min(a.n_seqs, (int)(blockIdx.z + 1) * s_per_block);
+    for (int s0 = blockIdx.z * s_per_block; s0 < s_end; s0 += 16) {
+        const int s = min(s0 + n, a.n_seqs - 1);
+        const __bf16* q = (const __bf16*)a.q + ((int64_t)s * H + h) * (HD + kRopeDim);
+        bf16x8 qf[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const bf16x8*)(q + 32 * ks + 8 * g);
+        __bf16* to = (__bf16*)a.q_lat + ((int64_t)s * H + h) * KD;
+        f32x4 acc[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) acc[i] = mfma16(wf[ks][i], qf[ks], acc[i]);
+        }
+        if (s0 + n >= a.n_seqs) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {  // (bf16, as the products with the cache take it)
+            bf16x8 v;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = (__bf16)acc[i][j];
+            *(bf16x8*)(to + r0 + 8 * (4 * g + j)) = v;
+        }
+        if (r0 == 0) {
+            *(bf16x8*)(to + R + 8 * g) = *(const bf16x8*)(q + HD + 8 * g);
+            *(bf16x8*)(to + R + 32 + 8 * g) = *(const bf16x8*)(q + HD + 32 + 8 * g);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The attention.  A workgroup of 8 waves holds up to 64 query rows and takes 64 tokens (4 pages) at a time through LDS.  For the
+// scores, S^T = C Q^T, a wave owns a page and half of the rows (its queries stay in registers: 32 rows x 576 values are 144 of
+// them); for the product with the values, O^T = C^T P^T, it owns R / 8 of their columns and all rows.  K and V are the same
+// bytes, and LDS delivers them twice and once to the workgroup instead of once to each wave.  What the waves exchange is the rows'
+// maxima and P (bf16, in the layout in which the score product leaves it and the value product wants it).  V's operand is columns
+// of a token-major page: ds_read_b64_tr_b16 reads 4 tokens x 16 columns transposed.
+// ---------------------------------------------------------------------------
+constexpr int kDecodeWaves = 8;
+template <int R>
+struct DecodeSmem {
+    __bf16 tile[2][4][(R + kRopeDim) * 16];
+    bf16x4 p[4][4][64];  // [page][row tile][lane]
+    float mx[4][kLatentTileRows];
+    float sum[4][kLatentTileRows];
+};
+
+template <int R>
+DEV void fetch_half_page(const char* pages, int page, const __bf16* to, int half, int lane) {
+    constexpr int BYTES = (R + kRopeDim) * 32;
+    const char* base = pages + (int64_t)uniform(page) * BYTES + half * (BYTES / 2);
+    const unsigned lds = uniform(lds_address(to)) + half * (BYTES / 2);
+#pragma unroll
+    for (int i = 0; i < BYTES / 2048; ++i) load_to_lds(base, lane * 16 + i * 1024, lds + i * 1024);
+}
+
+template <int R, int NT>  // NT row tiles of 16
+DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const taper_latent_item& it, DecodeSmem<R>& sm) {
+    constexpr int KD = R + kRopeDim, JK = KD / 32, DT = R / 16 / kDecodeWaves, NS = (NT + 1) / 2;  // NS: row tiles of a wave's scores
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+    const int pg = wave & 3, k0 = (wave >> 2) * NS;  // page and first row tile of this wave's scores
+    const bool scores = k0 < NT;
+    const int32_t* row = a.bt + (int64_t)it.seq0 * a.bt_stride + it.page0;
+    const int last_page = (it.n_tokens + 15) / 16 - 1, n_tiles = (it.n_tokens + 63) / 64;
+    const char* pages = (const char*)a.pages;
+    const float c = sh.scale_log2e;
+
+    fetch_half_page<R>(pages, row[min(pg, last_page)], sm.tile[0][pg], wave >> 2, lane);
+    int next = row[min(4 + pg, last_page)];
+    bf16x8 qf[NS][JK];
+#pragma unroll
+    for (int k = 0; k < NS; ++k) {
+        const __bf16* q = (const __bf16*)a.q_lat + (int64_t)(it.row0 + min(16 * (k0 + k) + n, it.n_rows - 1)) * KD + 8 * g;
+#pragma unroll
+        for (int j = 0; j < JK; ++j) qf[k][j] = *(const bf16x8*)(q + 32 * j);
+    }
+    f32x4 O[NT][DT];
+    float m[NT], l[NS];  // running maxima of all rows; sums of this wave's page and rows
+#pragma unroll
+    for (int k = 0; k < NT; ++k) {
+        m[k] = -INFINITY;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) O[k][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll
+    for (int k = 0; k < NS; ++k) l[k] = 0.f;
+    for (int t = 0; t < n_tiles; ++t) {
+        wait_loads_and_meet<0>();  // tile t is here for all, and all are done with tile t - 1
+        if (t + 1 < n_tiles) {
+            fetch_half_page<R>(pages, next, sm.tile[(t + 1) & 1][pg], wave >> 2, lane);
+            next = row[min(4 * (t + 2) + pg, last_page)];
+        }
+        __bf16* const mine = sm.tile[t & 1][pg];
+        const int valid = it.n_tokens - 64 * t - 16 * pg;  // of this wave's page
+        if (it.n_tokens - 64 * t < 64) {  // what follows the last token may be anything: zeros, so that its zero weight meets no NaN
+            for (int i = lane + (wave >> 2) * 64; i < KD / 8 * 16; i += 128)
+                if ((i & 15) >= valid) *(u32x4*)(mine + i * 8) = u32x4{0, 0, 0, 0};
+            meet();
+        }
+        f32x4 s[NS];
+        if (scores) {
+#pragma unroll
+            for (int k = 0; k < NS; ++k) s[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < JK; ++j) {
+                const bf16x8 kf = *(const bf16x8*)(mine + (4 * j + g) * 128 + n * 8);
+#pragma unroll
+                for (int k = 0; k < NS; ++k) s[k] = mfma16(kf, qf[k][j], s[k]);
+                if (j % 6 == 5) __builtin_amdgcn_sched_barrier(0);  // (else the whole page is read ahead, into registers that are not there)
+            }
+#pragma unroll
+            for (int k = 0; k < NS; ++k) {
+                if (valid < 16)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[k][i] = 4 * g + i < valid ? s[k][i] : -INFINITY;
+                const float mx = max_lane_groups(fmaxf(fmaxf(s[k][0], s[k][1]), fmaxf(s[k][2], s[k][3])));
+                if (g == 0) sm.mx[pg][16 * (k0 + k) + n] = mx;
+            }
+        }
+        meet();
+        float alpha[NT];
+        bool higher = false;
+#pragma unroll
+        for (int k = 0; k < NT; ++k) {
+            const float mx = fmaxf(fmaxf(sm.mx[0][16 * k + n], sm.mx[1][16 * k + n]), fmaxf(sm.mx[2][16 * k + n], sm.mx[3][16 * k + n]));
+            const float mn = fmaxf(m[k], mx * c);
+            higher |= mn > m[k];
+            alpha[k] = fast_exp2(m[k] - mn);
+            m[k] = mn;
+        }
+        if (scores) {
+#pragma unroll
+            for (int k = 0; k < NS; ++k) {
+                const float mk = NT == NS || wave < 4 ? m[k] : m[NT - NS + k];
+                f32x4 p;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[i] = fast_exp2(fmaf(s[k][i], c, -mk));
+                l[k] = fmaf(l[k], NT == NS || wave < 4 ? alpha[k] : alpha[NT - NS + k], (p[0] + p[1]) + (p[2] + p[3]));
+                sm.p[pg][k0 + k][lane] = __builtin_convertvector(p, bf16x4);  // (weights of at most 1, in 8 bits each)
+            }
+        }
+        if (__any(higher)) {
+#pragma unroll
+            for (int k = 0; k < NT; ++k)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) O[k][d] *= alpha[k];
+        }
+        meet();
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            bf16x8 pf[NT];
+#pragma unroll
+            for (int k = 0; k < NT; ++k) pf[k] = cat(sm.p[2 * ks][k][lane], sm.p[2 * ks + 1][k][lane]);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                const int at = (wave * DT + d) * 256 + (lane >> 1 & 1) * 128 + (4 * g + (n >> 2)) * 8 + (lane & 1) * 4;
+                typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+                const bf16x4 v0 = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(sm.tile[t & 1][2 * ks] + at)));
+                const bf16x4 v1 = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(sm.tile[t & 1][2 * ks + 1] + at)));
+                const bf16x8 vf = cat(v0, v1);
+#pragma unroll
+                for (int k = 0; k < NT; ++k) O[k][d] = mfma16(vf, pf[k], O[k][d]);
+            }
+        }
+    }
+    // a row's sum: over the lane groups, and over the waves' pages
+    if (scores)
+#pragma unroll
+        for (int k = 0; k < NS; ++k) {
+            const float mine = sum_lane_groups(l[k]);
+            if (g == 0) sm.sum[pg][16 * (k0 + k) + n] = mine;
+        }
+    meet();
+#pragma unroll
+    for (int k = 0; k < NT; ++k) {
+        const int r = 16 * k + n;
+        if (r >= it.n_rows) continue;
+        const float total = (sm.sum[0][r] + sm.sum[1][r]) + (sm.sum[2][r] + sm.sum[3][r]), inv = 1.0f / total;
+        const int64_t at = it.part_row + r;
+        if (wave == 0 && g == 0) a.ml[at] = make_float2(m[k], total);
+        float* to = (float*)a.part + at * R + wave * (R / kDecodeWaves) + 4 * g;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) *(f32x4*)(to + 16 * d) = O[k][d] * inv;
+    }
+}
+
+template <int R>
+__global__ __launch_bounds__(512, 2) void latent_decode_kernel(const LatentShape sh, const LatentDecodeArgs a) {
+    __shared__ DecodeSmem<R> sm;
+    const taper_latent_item it = a.items[blockIdx.x];
+    if (it.n_rows <= 0) return;
+    if (it.n_rows <= 16) decode_item<R, 1>(sh, a, it, sm);
+    else if (it.n_rows <= 32) decode_item<R, 2>(sh, a, it, sm);
+    else decode_item<R, 4>(sh, a, it, sm);
+}
+
+// ---------------------------------------------------------------------------
+// finish: merges the pieces of 16 sequences' rows of one head and applies W_v[h]: out^T = W_v O^T, W's rows straight from
+// memory (a lane's 16 bytes are 8 consecutive values of one row), the merged rows through LDS.
+// ---------------------------------------------------------------------------
+template <int R, int HD>
+__global__ __launch_bounds__(256) void finish_kernel(const LatentShape sh, const LatentDecodeArgs a) {
+    constexpr int PITCH = R + 8;
+    __shared__ __bf16 o[16][PITCH];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4, h = blockIdx.x, s0 = blockIdx.y * 16;
+    const int H = sh.n_heads;
+    for (int i = wave; i < 16; i += 4) {
+        const int s = s0 + i;
+        constexpr int PER = R / 64;
+        float acc[PER];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) acc[j] = 0.f;
+        if (s < a.n_seqs) {
+            const int b = a.piece_start[s], e = a.piece_start[s + 1];
+            float M = -INFINITY, L = 0.f;
+            for (int p = b + lane; p < e; p += 64) M = fmaxf(M, a.ml[a.piece_row[p] + h].x);
+            for (int d = 32; d; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
+            for (int p = b; p < e; ++p) {
+                const int64_t r = a.piece_row[p] + h;
+                const float2 ml = a.ml[r];
+                const float w = ml.y * fast_exp2(ml.x - M);
+                L += w;
+                const float* v = (const float*)a.part + r * R + lane * PER;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) acc[j] = fmaf(w, v[j], acc[j]);
+            }
+            const float inv = 1.0f / L;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) acc[j] *= inv;
+            if (a.lse && lane == 0) a.lse[(int64_t)s * H + h] = (M + log2f(L)) * 0.6931471805599453f;
+        }
+#pragma unroll
+        for (int j = 0; j < PER; ++j) o[i][lane * PER + j] = (__bf16)acc[j];  // (bf16, as W_v is)
+    }
+    __syncthreads();
+    constexpr int VT = HD / 64;  // 16-value tiles of a wave
+    const __bf16* w = (const __bf16*)a.w_up + ((int64_t)h * 2 + 1) * HD * R;
+#pragma unroll
+    for (int v = 0; v < VT; ++v) {
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        const int v0 = (wave * VT + v) * 16;
+#pragma unroll
+        for (int j = 0; j < R / 32; ++j)
+            acc = mfma16(*(const bf16x8*)(w + (int64_t)(v0 + n) * R + 32 * j + 8 * g), *(const bf16x8*)(&o[n][32 * j + 8 * g]), acc);
+        if (s0 + n < a.n_seqs) *(bf16x4*)((__bf16*)a.out + ((int64_t)(s0 + n) * H + h) * HD + v0 + 4 * g) = __builtin_convertvector(acc, bf16x4);
+    }
+}
+
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void latent_append_kernel(const __bf16* __restrict__ latent, const int64_t latent_stride,
+                                                            const __bf16* __restrict__ rope, const int64_t rope_stride,
+                                                            const int64_t* __restrict__ slots, __bf16* __restrict__ pages,
+                                                            const int64_t n, const int64_t n_slots, const int R) {
+    const int per = (R + kRopeDim) / 8;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n * per; i += (int64_t)gridDim.x * 256) {
+        const int64_t tok = i / per, slot = slots[tok];
+        const int d8 = (int)(i - tok * per);
+        if (slot < 0 || slot >= n_slots) continue;
+        const __bf16* from = 8 * d8 < R ? latent + tok * latent_stride + 8 * d8 : rope + tok * rope_stride + (8 * d8 - R);
+        *(bf16x8*)(pages + ((slot >> 4) * per + d8) * 128 + (slot & 15) * 8) = *(const bf16x8*)from;
+    }
+}
+
+}  // namespace latent
+
+using namespace latent;
+
+hipError_t launch_latent_append(int latent_dim, int64_t n, const void* latent, int64_t latent_stride, const void* rope, int64_t rope_stride,
+                                const int64_t* slots, void* pages, int64_t n_slots, hipStream_t s) {
+    const int64_t threads = n * ((latent_dim + kRopeDim) / 8);
+    const int64_t blocks = (threads + 255) / 256, most = 1 << 20;  // (a launch has fewer than 2^32 threads)
+    hipLaunchKernelGGL(latent_append_kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, s, (const __bf16*)latent, latent_stride,
+                       (const __bf16*)rope, rope_stride, slots, (__bf16*)pages, n, n_slots, latent_dim);
+    return hipGetLastError();
+}
+
+hipError_t launch_latent_decode(const LatentShape& sh, const LatentDecodeArgs& a, hipStream_t s) {
+    const int s_per_block = 64;
+    const dim3 grid(sh.n_heads, sh.latent_dim / 128, (a.n_seqs + s_per_block - 1) / s_per_block);
+    if (sh.head_dim == 128) hipLaunchKernelGGL((absorb_kernel<4>), grid, dim3(64), 0, s, sh, a, s_per_block);
+    else hipLaunchKernelGGL((absorb_kernel<2>), grid, dim3(64), 0, s, sh, a, s_per_block);
+    if (sh.latent_dim == 512) hipLaunchKernelGGL((latent_decode_kernel<512>), dim3(a.n_items), dim3(64 * kDecodeWaves), 0, s, sh, a);
+    else hipLaunchKernelGGL((latent_decode_kernel<256>), dim3(a.n_items), dim3(64 * kDecodeWaves), 0, s, sh, a);
+    const dim3 fgrid(sh.n_heads, (a.n_seqs + 15) / 16);
+    if (sh.latent_dim == 512 && sh.head_dim == 128) hipLaunchKernelGGL((finish_kernel<512, 128>), fgrid, dim3(256), 0, s, sh, a);
+    else if (sh.latent_dim == 512) hipLaunchKernelGGL((finish_kernel<512, 64>), fgrid, dim3(256), 0, s, sh, a);
+    else if (sh.head_dim == 128) hipLaunchKernelGGL((finish_kernel<256, 128>), fgrid, dim3(256), 0, s, sh, a);
+    else hipLaunchKernelGGL((finish_kernel<256, 64>), fgrid, dim3(256), 0, s, sh, a);
+    return hipGetLastError();
+}
+
+}  // namespace taper

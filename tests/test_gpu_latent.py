@@ -1,0 +1,142 @@
+"""Latent-cache attention (decode step and prompts) and append on the GPU against the definition in 64 bits."""
+import numpy as np
+import pytest
+
+from tests.latent_ref import RMS, ROPE, Batch, attention, pool_of, rows_of, to_bf16, values
+
+pytestmark = pytest.mark.gpu
+
+
+def dev(x, dtype=None):
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(x)).to("cuda:0")
+    return t.to(torch.bfloat16) if dtype is None and t.dtype == torch.float32 else t
+
+
+def context(H, R, hd, **kw):
+    from paper_2605_06914_amd import LatentContext
+    return LatentContext(H, R, hd, device=0, **kw)
+
+
+def plan_of(ctx, b, prompt=False, **kw):
+    if prompt:
+        return ctx.prompt_plan_build(b.table, b.group, b.prefix, b.seg_len, b.new, b.n_pages)
+    return ctx.plan_build(b.table, b.group, b.prefix, b.seg_len, b.n_pages, seg_start=b.seg_start, **kw)
+
+
+def run(ctx, b, q, w, tok, prompt=False, plan=None, stream=None, **kw):
+    import torch
+    q_d, w_d, pages = dev(q), dev(w), dev(pool_of(tok))
+    H, hd = w.shape[0], w.shape[1] // 2
+    out = torch.full((q.shape[0], H, hd), float("nan"), dtype=torch.bfloat16, device="cuda:0")
+    lse = torch.full((q.shape[0], H), float("nan"), device="cuda:0")
+    plan = plan or plan_of(ctx, b, prompt, **kw)
+    (ctx.prompt_attention if prompt else ctx.decode_step_attention)(plan, q_d, w_d, pages, out, lse)
+    torch.cuda.synchronize()
+    return out.double().cpu().numpy(), lse.double().cpu().numpy()
+
+
+def check(got, want, what):
+    (out, lse), (ref, ref_lse, tol, tol_lse) = got, want
+    assert np.isfinite(out).all() and np.isfinite(lse).all(), what
+    err, rms = np.abs(out - ref), float(np.sqrt(np.mean(ref ** 2)))
+    print(f"[latent] {what}: max {err.max():.2e} (bound there {tol.flat[err.argmax()]:.2e}), rms {np.sqrt(np.mean(err ** 2)) / rms:.2e} of the result's", flush=True)
+    assert (err <= tol).all(), f"{what}: {np.argwhere(err > tol)[:5]}"
+    assert np.sqrt(np.mean(err ** 2)) <= RMS * rms, what
+    assert (np.abs(lse - ref_lse) <= tol_lse).all(), what
+
+
+SHAPES = [(16, 512, 128), (128, 512, 128), (20, 512, 64), (5, 256, 64), (1, 256, 128), (64, 256, 128)]
+SERIAL = [(0, [[n]]) for n in (1, 15, 16, 17, 63, 64, 65, 130, 300)] + [(n, [[0]]) for n in (1, 33, 64, 129)]
+BRANCHES = [(37, [[0], [1], [16], [70]]), (64, [[5]] * 3), (0, [[9]]), (200, [[3], [0]]), (1, [[1]] * 5)]
+
+
+@pytest.mark.parametrize("H,R,hd", SHAPES)
+@pytest.mark.parametrize("requests", [SERIAL, BRANCHES], ids=["serial", "branches"])
+def test_decode_step(H, R, hd, requests):
+    b = Batch(requests, 1)
+    q, w, tok = values(b, H, R, hd, 2)
+    ctx = context(H, R, hd)
+    check(run(ctx, b, q, w, tok), attention(b, q, w, tok, H, R, hd, (hd + ROPE) ** -0.5, True), f"decode H {H} R {R} hd {hd}")
+
+
+@pytest.mark.parametrize("workgroups", [1, 7, 64, 4096])
+def test_decode_step_cut_in_other_ways(workgroups):
+    """One long context and a wide request, cut for few and for many workgroups."""
+    H, R, hd = 24, 512, 128
+    b = Batch([(0, [[2500]]), (700, [[n] for n in range(0, 36, 3)]), (40, [[100, 0, 31], [2, 2]])], 3)
+    q, w, tok = values(b, H, R, hd, 4)
+    ctx = context(H, R, hd, scale=0.11)
+    check(run(ctx, b, q, w, tok, target_workgroups=workgroups), attention(b, q, w, tok, H, R, hd, 0.11, True), f"{workgroups} workgroups")
+
+
+def test_decode_step_is_the_same_every_time_and_branches_do_not_see_each_other():
+    H, R, hd = 32, 512, 128
+    b = Batch([(900, [[10], [200], [40]]), (0, [[333]])], 5)
+    q, w, tok = values(b, H, R, hd, 6)
+    ctx = context(H, R, hd)
+    first = run(ctx, b, q, w, tok)
+    for _ in range(5):
+        again = run(ctx, b, q, w, tok)
+        assert np.array_equal(first[0], again[0]) and np.array_equal(first[1], again[1])
+    other = tok.copy()
+    other[b.slots(1)[900:]] = 3.0  # a sibling's own tokens
+    changed = run(ctx, b, q, w, other)
+    assert np.array_equal(first[0][[0, 2, 3]], changed[0][[0, 2, 3]]) and not np.array_equal(first[0][1], changed[0][1])
+
+
+def test_scores_far_apart_and_equal_ones():
+    """Scores of some hundreds (one token has all the weight), and all equal."""
+    H, R, hd = 16, 256, 64
+    b = Batch([(70, [[40], [0]])], 7)
+    q, w, tok = values(b, H, R, hd, 8)
+    live = b.slots(0)
+    q[0] *= 64
+    q[1] = 0
+    want = attention(b, q, w, tok, H, R, hd, (hd + ROPE) ** -0.5, True)
+    out, lse = run(context(H, R, hd), b, q, w, tok)
+    assert np.isfinite(out).all()
+    mean = tok[live[:70], :R].astype(np.float64).mean(0)
+    ref = np.einsum("hvr,r->hv", w[:, hd:].astype(np.float64), mean)
+    assert (np.abs(out[1] - ref) <= want[2][1]).all()
+    assert (np.abs(out - want[0]) <= want[2]).all()
+
+
+@pytest.mark.parametrize("H,R,hd", SHAPES)
+def test_prompts_of_ragged_lengths(H, R, hd):
+    requests = [(0, [[n]]) for n in (1, 2, 15, 16, 17, 64, 127, 128, 129, 200)] + [(0, [[90]]), (0, [[300]])]
+    b = Batch(requests, 9, new=[1, 2, 15, 16, 17, 64, 127, 128, 129, 200, 0, 7])
+    q, w, tok = values(b, H, R, hd, 10)
+    check(run(context(H, R, hd), b, q, w, tok, True), attention(b, q, w, tok, H, R, hd, (hd + ROPE) ** -0.5, False), f"prompts H {H} R {R} hd {hd}")
+
+
+@pytest.mark.parametrize("H,R,hd", [(16, 512, 128), (5, 256, 64)])
+def test_prompts_behind_cached_tokens_and_shared_prefixes(H, R, hd):
+    requests = [(100, [[20], [1], [150], [0]]), (16, [[16], [5]]), (1, [[1]]), (0, [[700]]), (63, [[65]])]
+    b = Batch(requests, 11, new=[20, 1, 130, 0, 3, 5, 1, 33, 64])
+    q, w, tok = values(b, H, R, hd, 12)
+    check(run(context(H, R, hd), b, q, w, tok, True), attention(b, q, w, tok, H, R, hd, (hd + ROPE) ** -0.5, False), f"prefixes H {H} R {R} hd {hd}")
+
+
+@pytest.mark.parametrize("n,R,wide", [(1, 512, False), (37, 256, True), (5000, 512, True), (0, 512, False)])
+def test_append_writes_its_slots_and_nothing_else(n, R, wide):
+    import torch
+    rng = np.random.default_rng(n)
+    n_pages = n // 16 + 4
+    before = to_bf16(rng.standard_normal((n_pages * 16, R + ROPE)))
+    rows = to_bf16(rng.standard_normal((n, R + ROPE + (64 if wide else 0))))
+    slots = rng.permutation(n_pages * 16)[:n].astype(np.int64)
+    if n > 4:
+        slots[1::4] = -1
+        slots[2] = n_pages * 16  # behind the pool
+    pages, rows_d = dev(pool_of(before)), dev(rows)
+    ctx = context(16, R, 128)
+    if wide:
+        latent, rope = rows_d[:, 64:64 + R], rows_d[:, 64 + R:]
+    else:
+        latent, rope = rows_d[:, :R].contiguous(), rows_d[:, R:].contiguous()
+    ctx.append(latent, rope, dev(slots), pages, n_pages)
+    torch.cuda.synchronize()
+    keep = (slots >= 0) & (slots < n_pages * 16)
+    before[slots[keep]] = rows[keep][:, -(R + ROPE):]
+    assert np.array_equal(rows_of(pages.float().cpu().numpy()), before)
