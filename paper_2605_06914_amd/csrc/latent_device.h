@@ -8,6 +8,8 @@ namespace latent {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
@@ -18,13 +20,17 @@ DEV f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32
 DEV float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 DEV bf16x8 cat(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
+// (maximum, not maxnum: it takes its values as they are, where maxnum first quiets each; a NaN makes its row NaN.)
+DEV float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+DEV float max4(f32x4 v) { return max2(max2(v[0], v[1]), max2(v[2], v[3])); }
+
 // A row of scores lives in lanes n, n + 16, n + 32, n + 48: these bring its four parts together by lane swaps.
 DEV float max_lane_groups(float v) {
     unsigned u = __float_as_uint(v);
     auto p = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    u = __float_as_uint(fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])));
+    u = __float_as_uint(max2(__uint_as_float(p[0]), __uint_as_float(p[1])));
     p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    return max2(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 DEV float sum_lane_groups(float v) {
     unsigned u = __float_as_uint(v);
@@ -50,6 +56,9 @@ DEV void wait_loads_and_meet() {
 }
 // LDS accesses are done and every wave is here; loads stay in flight.
 DEV void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Integers of a plan, which no kernel writes: read by scalar loads.
+typedef const __attribute__((address_space(4))) int32_t* scalar_row;
 
 DEV int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 

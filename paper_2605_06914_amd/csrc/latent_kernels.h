@@ -17,14 +17,19 @@ struct LatentShape {
     float scale_log2e;  // scale * log2(e)
 };
 
+struct PartStats {             // of a partial row
+    float m, l;               // running max in log2 units, sum
+    signed char exponent[8];  // of each eighth of its columns
+};
 struct LatentDecodeArgs {
     const int32_t* bt;              // [n_seqs][bt_stride]
     const taper_latent_item* items;
     const int32_t* piece_start;     // [n_seqs + 1]
     const int32_t* piece_row;
     void* q_lat;                    // bf16 [n_seqs * n_heads][latent_dim + 64]
-    float2* ml;                     // [n_partial_rows] running max in log2 units, sum
-    void* part;                     // [n_partial_rows][latent_dim] rows divided by their own sum
+    void* q_rest;                   // bf16 [n_seqs * n_heads][latent_dim]: what q_lat's rounding took away (written where lse is wanted)
+    PartStats* stats;               // [n_partial_rows]
+    void* part;                     // f16 [n_partial_rows][latent_dim]: rows divided by their own sum and their columns' powers of two
     const void* q;
     const void* w_up;
     const void* pages;

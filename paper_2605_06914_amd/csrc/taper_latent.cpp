@@ -277,8 +277,9 @@ int build_decode(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, 
     lay.add(plan->piece_row.data(), plan->piece_row.size() * 4);
     const size_t image = lay.total();
     lay.add(nullptr, (size_t)n_seqs * cfg.n_heads * KD * 2);
-    lay.add(nullptr, (size_t)plan->n_partial_rows * sizeof(float2));
-    lay.add(nullptr, (size_t)plan->n_partial_rows * cfg.latent_dim * sizeof(float));
+    lay.add(nullptr, (size_t)n_seqs * cfg.n_heads * cfg.latent_dim * 2);
+    lay.add(nullptr, (size_t)plan->n_partial_rows * sizeof(taper::PartStats));
+    lay.add(nullptr, (size_t)plan->n_partial_rows * cfg.latent_dim * 2);
     plan->device_bytes = (int64_t)lay.total();
     if (cfg.device < 0) return TAPER_OK;
     const int su = upload(plan, lay, image, s);
@@ -291,8 +292,9 @@ int build_decode(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, 
     a.piece_start = (const int32_t*)lay.at(d, 2);
     a.piece_row = (const int32_t*)lay.at(d, 3);
     a.q_lat = lay.at(d, 4);
-    a.ml = (float2*)lay.at(d, 5);
-    a.part = lay.at(d, 6);
+    a.q_rest = lay.at(d, 5);
+    a.stats = (taper::PartStats*)lay.at(d, 6);
+    a.part = lay.at(d, 7);
     a.bt_stride = stride;
     a.n_seqs = n_seqs;
     a.n_items = (int32_t)plan->items.size();

@@ -59,6 +59,11 @@ __global__ __launch_bounds__(64) void absorb_kernel(const LatentShape sh, const 
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = (__bf16)acc[i][j];
             *(bf16x8*)(to + r0 + 8 * (4 * g + j)) = v;
+            if (a.lse) {  // what the rounding took away: finish_kernel puts its effect on the normaliser back
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = (__bf16)(acc[i][j] - (float)v[i]);
+                *(bf16x8*)((__bf16*)a.q_rest + ((int64_t)s * H + h) * R + r0 + 8 * (4 * g + j)) = v;
+            }
         }
         if (r0 == 0) {
             *(bf16x8*)(to + R + 8 * g) = *(const bf16x8*)(q + HD + 8 * g);
@@ -72,16 +77,24 @@ __global__ __launch_bounds__(64) void absorb_kernel(const LatentShape sh, const 
 // scores, S^T = C Q^T, a wave owns a page and half of the rows (its queries stay in registers: 32 rows x 576 values are 144 of
 // them); for the product with the values, O^T = C^T P^T, it owns R / 8 of their columns and all rows.  K and V are the same
 // bytes, and LDS delivers them twice and once to the workgroup instead of once to each wave.  What the waves exchange is the rows'
-// maxima and P (bf16, in the layout in which the score product leaves it and the value product wants it).  V's operand is columns
+// maxima and P (bf16, in the layout in which the score product leaves it and the value product wants it; it takes the place of the
+// page's rotated parts, which are of no more use then).  V's operand is columns
 // of a token-major page: ds_read_b64_tr_b16 reads 4 tokens x 16 columns transposed.
 // ---------------------------------------------------------------------------
 constexpr int kDecodeWaves = 8;
+// A partial row travels divided by its own sum, in half precision after division by a power of two of each wave's R / 8 columns that
+// brings their largest magnitude into [0.5, 1): off by 2^-12 of that, whatever the magnitude, and half the bytes of fp32 rows.
+DEV int exponent_of(float most) {
+    const int e = (int)((__float_as_uint(most) >> 23) & 0xff) - 126;
+    return e < -126 ? -126 : (e > 126 ? 126 : e);
+}
 template <int R>
 struct DecodeSmem {
+    // (the small ones first: an LDS access has 16 bits of offset, and addresses beyond it cost a register each)
+    f32x4 mx[kLatentTileRows];   // a row's maximum in each of the four pages
+    f32x4 sum[kLatentTileRows];
+    bf16x8 q_rope[4][2][64];     // [row tile][k-step][lane]: the queries' rotated parts (the rest is in registers, which these would not fit)
     __bf16 tile[2][4][(R + kRopeDim) * 16];
-    bf16x4 p[4][4][64];  // [page][row tile][lane]
-    float mx[4][kLatentTileRows];
-    float sum[4][kLatentTileRows];
 };
 
 template <int R>
@@ -90,28 +103,32 @@ DEV void fetch_half_page(const char* pages, int page, const __bf16* to, int half
     const char* base = pages + (int64_t)uniform(page) * BYTES + half * (BYTES / 2);
     const unsigned lds = uniform(lds_address(to)) + half * (BYTES / 2);
 #pragma unroll
-    for (int i = 0; i < BYTES / 2048; ++i) load_to_lds(base, lane * 16 + i * 1024, lds + i * 1024);
+    for (int i = 0; i < BYTES / 2048; ++i) load_to_lds(base + i * 1024, lane * 16, lds + i * 1024);  // (scalar sums: one lane offset for all)
 }
 
 template <int R, int NT>  // NT row tiles of 16
 DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const taper_latent_item& it, DecodeSmem<R>& sm) {
-    constexpr int KD = R + kRopeDim, JK = KD / 32, DT = R / 16 / kDecodeWaves, NS = (NT + 1) / 2;  // NS: row tiles of a wave's scores
+    constexpr int KD = R + kRopeDim, JL = R / 32, DT = R / 16 / kDecodeWaves, NS = (NT + 1) / 2;  // NS: row tiles of a wave's scores
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     const int pg = wave & 3, k0 = (wave >> 2) * NS;  // page and first row tile of this wave's scores
     const bool scores = k0 < NT;
-    const int32_t* row = a.bt + (int64_t)it.seq0 * a.bt_stride + it.page0;
+    const scalar_row row = (scalar_row)(a.bt + (int64_t)it.seq0 * a.bt_stride + it.page0);
     const int last_page = (it.n_tokens + 15) / 16 - 1, n_tiles = (it.n_tokens + 63) / 64;
     const char* pages = (const char*)a.pages;
     const float c = sh.scale_log2e;
 
     fetch_half_page<R>(pages, row[min(pg, last_page)], sm.tile[0][pg], wave >> 2, lane);
     int next = row[min(4 + pg, last_page)];
-    bf16x8 qf[NS][JK];
+    bf16x8 qf[NS][JL];
 #pragma unroll
     for (int k = 0; k < NS; ++k) {
         const __bf16* q = (const __bf16*)a.q_lat + (int64_t)(it.row0 + min(16 * (k0 + k) + n, it.n_rows - 1)) * KD + 8 * g;
 #pragma unroll
-        for (int j = 0; j < JK; ++j) qf[k][j] = *(const bf16x8*)(q + 32 * j);
+        for (int j = 0; j < JL; ++j) qf[k][j] = *(const bf16x8*)(q + 32 * j);
+        if (pg == 0 && scores) {
+            sm.q_rope[k0 + k][0][lane] = *(const bf16x8*)(q + R);
+            sm.q_rope[k0 + k][1][lane] = *(const bf16x8*)(q + R + 32);
+        }
     }
     f32x4 O[NT][DT];
     float m[NT], l[NS];  // running maxima of all rows; sums of this wave's page and rows
@@ -141,19 +158,25 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
 #pragma unroll
             for (int k = 0; k < NS; ++k) s[k] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < JK; ++j) {
+            for (int j = 0; j < JL; ++j) {
                 const bf16x8 kf = *(const bf16x8*)(mine + (4 * j + g) * 128 + n * 8);
 #pragma unroll
                 for (int k = 0; k < NS; ++k) s[k] = mfma16(kf, qf[k][j], s[k]);
-                if (j % 6 == 5) __builtin_amdgcn_sched_barrier(0);  // (else the whole page is read ahead, into registers that are not there)
+                if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (else the whole page is read ahead, into registers that are not there)
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const bf16x8 kf = *(const bf16x8*)(mine + (R / 8 + 4 * j + g) * 128 + n * 8);
+#pragma unroll
+                for (int k = 0; k < NS; ++k) s[k] = mfma16(kf, sm.q_rope[k0 + k][j][lane], s[k]);
             }
 #pragma unroll
             for (int k = 0; k < NS; ++k) {
                 if (valid < 16)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[k][i] = 4 * g + i < valid ? s[k][i] : -INFINITY;
-                const float mx = max_lane_groups(fmaxf(fmaxf(s[k][0], s[k][1]), fmaxf(s[k][2], s[k][3])));
-                if (g == 0) sm.mx[pg][16 * (k0 + k) + n] = mx;
+                const float mx = max_lane_groups(max4(s[k]));
+                if (g == 0) ((float*)&sm.mx[16 * (k0 + k) + n])[pg] = mx;
             }
         }
         meet();
@@ -161,8 +184,9 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
         bool higher = false;
 #pragma unroll
         for (int k = 0; k < NT; ++k) {
-            const float mx = fmaxf(fmaxf(sm.mx[0][16 * k + n], sm.mx[1][16 * k + n]), fmaxf(sm.mx[2][16 * k + n], sm.mx[3][16 * k + n]));
-            const float mn = fmaxf(m[k], mx * c);
+            const f32x4 of = sm.mx[16 * k + n];
+            const float mx = max4(of);
+            const float mn = max2(m[k], mx * c);
             higher |= mn > m[k];
             alpha[k] = fast_exp2(m[k] - mn);
             m[k] = mn;
@@ -175,7 +199,7 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
 #pragma unroll
                 for (int i = 0; i < 4; ++i) p[i] = fast_exp2(fmaf(s[k][i], c, -mk));
                 l[k] = fmaf(l[k], NT == NS || wave < 4 ? alpha[k] : alpha[NT - NS + k], (p[0] + p[1]) + (p[2] + p[3]));
-                sm.p[pg][k0 + k][lane] = __builtin_convertvector(p, bf16x4);  // (weights of at most 1, in 8 bits each)
+                ((bf16x4*)(mine + R * 16))[(k0 + k) * 64 + lane] = __builtin_convertvector(p, bf16x4);  // (weights of at most 1, in 8 bits each)
             }
         }
         if (__any(higher)) {
@@ -189,7 +213,8 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
         for (int ks = 0; ks < 2; ++ks) {
             bf16x8 pf[NT];
 #pragma unroll
-            for (int k = 0; k < NT; ++k) pf[k] = cat(sm.p[2 * ks][k][lane], sm.p[2 * ks + 1][k][lane]);
+            for (int k = 0; k < NT; ++k)
+                pf[k] = cat(((const bf16x4*)(sm.tile[t & 1][2 * ks] + R * 16))[k * 64 + lane], ((const bf16x4*)(sm.tile[t & 1][2 * ks + 1] + R * 16))[k * 64 + lane]);
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
                 const int at = (wave * DT + d) * 256 + (lane >> 1 & 1) * 128 + (4 * g + (n >> 2)) * 8 + (lane & 1) * 4;
@@ -207,19 +232,34 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
 #pragma unroll
         for (int k = 0; k < NS; ++k) {
             const float mine = sum_lane_groups(l[k]);
-            if (g == 0) sm.sum[pg][16 * (k0 + k) + n] = mine;
+            if (g == 0) ((float*)&sm.sum[16 * (k0 + k) + n])[pg] = mine;
         }
     meet();
 #pragma unroll
     for (int k = 0; k < NT; ++k) {
         const int r = 16 * k + n;
         if (r >= it.n_rows) continue;
-        const float total = (sm.sum[0][r] + sm.sum[1][r]) + (sm.sum[2][r] + sm.sum[3][r]), inv = 1.0f / total;
+        const f32x4 of = sm.sum[r];
+        const float total = (of[0] + of[1]) + (of[2] + of[3]), inv = 1.0f / total;
         const int64_t at = it.part_row + r;
-        if (wave == 0 && g == 0) a.ml[at] = make_float2(m[k], total);
-        float* to = (float*)a.part + at * R + wave * (R / kDecodeWaves) + 4 * g;
+        float most = 0.f;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) *(f32x4*)(to + 16 * d) = O[k][d] * inv;
+        for (int d = 0; d < DT; ++d) {
+            O[k][d] *= inv;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(O[k][d][i]));
+        }
+        const int e = exponent_of(max_lane_groups(most));
+        PartStats* const st = a.stats + at;
+        if (g == 0) st->exponent[wave] = (signed char)e;
+        if (wave == 0 && g == 0) {
+            st->m = m[k];
+            st->l = total;
+        }
+        _Float16* to = (_Float16*)a.part + at * R + wave * (R / kDecodeWaves) + 4 * g;
+        const float down = __uint_as_float((unsigned)(127 - e) << 23);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) *(f16x4*)(to + 16 * d) = __builtin_convertvector(O[k][d] * down, f16x4);
     }
 }
 
@@ -234,55 +274,95 @@ __global__ __launch_bounds__(512, 2) void latent_decode_kernel(const LatentShape
 }
 
 // ---------------------------------------------------------------------------
-// finish: merges the pieces of 16 sequences' rows of one head and applies W_v[h]: out^T = W_v O^T, W's rows straight from
-// memory (a lane's 16 bytes are 8 consecutive values of one row), the merged rows through LDS.
+// finish: merges the pieces of SB sequences' rows of one head and applies W_v[h]: out^T = W_v O^T, W's rows straight from memory
+// (a lane's 16 bytes are 8 consecutive values of one row; asked for before the merge, whose reads they overlap), the merged rows
+// through LDS as a sum of two bf16 values each, so that they are not rounded to one.
 // ---------------------------------------------------------------------------
-template <int R, int HD>
-__global__ __launch_bounds__(256) void finish_kernel(const LatentShape sh, const LatentDecodeArgs a) {
-    constexpr int PITCH = R + 8;
-    __shared__ __bf16 o[16][PITCH];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4, h = blockIdx.x, s0 = blockIdx.y * 16;
+template <int R, int HD, int SB>
+__global__ __launch_bounds__(512) void finish_kernel(const LatentShape sh, const LatentDecodeArgs a) {
+    constexpr int PITCH = R + 8, PER = R * SB / 512, UN = 4;  // PER: columns of a thread; UN: pieces in flight
+    typedef _Float16 part_t __attribute__((ext_vector_type(PER)));
+    __shared__ __align__(16) __bf16 o[2][SB][PITCH];
+    __shared__ float dots[SB][2], norm[SB];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4, h = blockIdx.x, s0 = blockIdx.y * SB;
     const int H = sh.n_heads;
-    for (int i = wave; i < 16; i += 4) {
-        const int s = s0 + i;
-        constexpr int PER = R / 64;
+    constexpr int VT = HD / 16;  // waves with a tile of 16 values
+    const __bf16* w = (const __bf16*)a.w_up + ((int64_t)h * 2 + 1) * HD * R + (int64_t)(wave * 16 + n) * R + 8 * g;
+    bf16x8 wf[R / 32];
+    if (wave < VT)
+#pragma unroll
+        for (int j = 0; j < R / 32; ++j) wf[j] = *(const bf16x8*)(w + 32 * j);
+    {
+        const int i = tid / (512 / SB), d0 = tid % (512 / SB) * PER, s = s0 + i, chunk = d0 / (R / kDecodeWaves);
         float acc[PER];
 #pragma unroll
         for (int j = 0; j < PER; ++j) acc[j] = 0.f;
         if (s < a.n_seqs) {
             const int b = a.piece_start[s], e = a.piece_start[s + 1];
             float M = -INFINITY, L = 0.f;
-            for (int p = b + lane; p < e; p += 64) M = fmaxf(M, a.ml[a.piece_row[p] + h].x);
-            for (int d = 32; d; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
-            for (int p = b; p < e; ++p) {
-                const int64_t r = a.piece_row[p] + h;
-                const float2 ml = a.ml[r];
-                const float w = ml.y * fast_exp2(ml.x - M);
-                L += w;
-                const float* v = (const float*)a.part + r * R + lane * PER;
+            for (int p = b; p < e; p += UN) {
 #pragma unroll
-                for (int j = 0; j < PER; ++j) acc[j] = fmaf(w, v[j], acc[j]);
+                for (int u = 0; u < UN; ++u) M = fmaxf(M, a.stats[a.piece_row[min(p + u, e - 1)] + h].m);
+            }
+            for (int p = b; p < e; p += UN) {
+                part_t v[UN];
+                float2 ml[UN];
+                int ex[UN];
+#pragma unroll
+                for (int u = 0; u < UN; ++u) {
+                    const int64_t r = a.piece_row[min(p + u, e - 1)] + h;
+                    ml[u] = *(const float2*)&a.stats[r];
+                    ex[u] = a.stats[r].exponent[chunk];
+                    v[u] = *(const part_t*)((const _Float16*)a.part + r * R + d0);
+                }
+#pragma unroll
+                for (int u = 0; u < UN; ++u) {
+                    const float wt = p + u < e ? ml[u].y * fast_exp2(ml[u].x - M) : 0.f;
+                    L += wt;
+                    const float up = wt * __uint_as_float((unsigned)(127 + ex[u]) << 23);
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) acc[j] = p + u < e ? fmaf(up, (float)v[u][j], acc[j]) : acc[j];
+                }
             }
             const float inv = 1.0f / L;
 #pragma unroll
             for (int j = 0; j < PER; ++j) acc[j] *= inv;
-            if (a.lse && lane == 0) a.lse[(int64_t)s * H + h] = (M + log2f(L)) * 0.6931471805599453f;
+            if (a.lse) {
+                // The scores were made with rounded queries: to first order the normaliser is off by the weighted mean of the scores'
+                // errors, scale (q - rounded q) . (sum_t p_t c_t).
+                const __bf16* rest = (const __bf16*)a.q_rest + ((int64_t)s * H + h) * R + d0;
+                float dot = 0.f;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) dot = fmaf((float)rest[j], acc[j], dot);
+                constexpr int LANES = 512 / SB < 64 ? 512 / SB : 64;
+#pragma unroll
+                for (int x = LANES / 2; x; x >>= 1) dot += __shfl_xor(dot, x);
+                if (lane % LANES == 0) dots[i][tid % (512 / SB) / 64] = dot;
+                if (d0 == 0) norm[i] = M + log2f(L);
+            }
         }
 #pragma unroll
-        for (int j = 0; j < PER; ++j) o[i][lane * PER + j] = (__bf16)acc[j];  // (bf16, as W_v is)
+        for (int j = 0; j < PER; ++j) {
+            const __bf16 hi = (__bf16)acc[j];
+            o[0][i][d0 + j] = hi;
+            o[1][i][d0 + j] = (__bf16)(acc[j] - (float)hi);
+        }
     }
     __syncthreads();
-    constexpr int VT = HD / 64;  // 16-value tiles of a wave
-    const __bf16* w = (const __bf16*)a.w_up + ((int64_t)h * 2 + 1) * HD * R;
-#pragma unroll
-    for (int v = 0; v < VT; ++v) {
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        const int v0 = (wave * VT + v) * 16;
-#pragma unroll
-        for (int j = 0; j < R / 32; ++j)
-            acc = mfma16(*(const bf16x8*)(w + (int64_t)(v0 + n) * R + 32 * j + 8 * g), *(const bf16x8*)(&o[n][32 * j + 8 * g]), acc);
-        if (s0 + n < a.n_seqs) *(bf16x4*)((__bf16*)a.out + ((int64_t)(s0 + n) * H + h) * HD + v0 + 4 * g) = __builtin_convertvector(acc, bf16x4);
+    if (a.lse && tid < SB && s0 + tid < a.n_seqs) {
+        float dot = 0.f;
+        for (int x = 0; x < (512 / SB + 63) / 64; ++x) dot += dots[tid][x];
+        a.lse[(int64_t)(s0 + tid) * H + h] = (norm[tid] + dot * sh.scale_log2e) * 0.6931471805599453f;
     }
+    if (wave >= VT) return;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < R / 32; ++j) {
+        acc = mfma16(wf[j], *(const bf16x8*)(&o[1][n % SB][32 * j + 8 * g]), acc);
+        acc = mfma16(wf[j], *(const bf16x8*)(&o[0][n % SB][32 * j + 8 * g]), acc);
+    }
+    if (n < SB && s0 + n < a.n_seqs)
+        *(bf16x4*)((__bf16*)a.out + ((int64_t)(s0 + n) * H + h) * HD + wave * 16 + 4 * g) = __builtin_convertvector(acc, bf16x4);
 }
 
 // ---------------------------------------------------------------------------
@@ -313,6 +393,12 @@ hipError_t launch_latent_append(int latent_dim, int64_t n, const void* latent, i
     return hipGetLastError();
 }
 
+template <int R, int HD>
+static void launch_finish(bool many, const LatentShape& sh, const LatentDecodeArgs& a, hipStream_t s) {
+    if (many) hipLaunchKernelGGL((finish_kernel<R, HD, 16>), dim3(sh.n_heads, (a.n_seqs + 15) / 16), dim3(512), 0, s, sh, a);
+    else hipLaunchKernelGGL((finish_kernel<R, HD, 4>), dim3(sh.n_heads, (a.n_seqs + 3) / 4), dim3(512), 0, s, sh, a);
+}
+
 hipError_t launch_latent_decode(const LatentShape& sh, const LatentDecodeArgs& a, hipStream_t s) {
     const int s_per_block = 64;
     const dim3 grid(sh.n_heads, sh.latent_dim / 128, (a.n_seqs + s_per_block - 1) / s_per_block);
@@ -320,11 +406,12 @@ hipError_t launch_latent_decode(const LatentShape& sh, const LatentDecodeArgs& a
     else hipLaunchKernelGGL((absorb_kernel<2>), grid, dim3(64), 0, s, sh, a, s_per_block);
     if (sh.latent_dim == 512) hipLaunchKernelGGL((latent_decode_kernel<512>), dim3(a.n_items), dim3(64 * kDecodeWaves), 0, s, sh, a);
     else hipLaunchKernelGGL((latent_decode_kernel<256>), dim3(a.n_items), dim3(64 * kDecodeWaves), 0, s, sh, a);
-    const dim3 fgrid(sh.n_heads, (a.n_seqs + 15) / 16);
-    if (sh.latent_dim == 512 && sh.head_dim == 128) hipLaunchKernelGGL((finish_kernel<512, 128>), fgrid, dim3(256), 0, s, sh, a);
-    else if (sh.latent_dim == 512) hipLaunchKernelGGL((finish_kernel<512, 64>), fgrid, dim3(256), 0, s, sh, a);
-    else if (sh.head_dim == 128) hipLaunchKernelGGL((finish_kernel<256, 128>), fgrid, dim3(256), 0, s, sh, a);
-    else hipLaunchKernelGGL((finish_kernel<256, 64>), fgrid, dim3(256), 0, s, sh, a);
+    // Sixteen sequences a workgroup read W_v once for all of them; where that leaves most of the chip idle, four.
+    const bool many = (int64_t)sh.n_heads * ((a.n_seqs + 15) / 16) >= 256;
+    if (sh.latent_dim == 512 && sh.head_dim == 128) launch_finish<512, 128>(many, sh, a, s);
+    else if (sh.latent_dim == 512) launch_finish<512, 64>(many, sh, a, s);
+    else if (sh.head_dim == 128) launch_finish<256, 128>(many, sh, a, s);
+    else launch_finish<256, 64>(many, sh, a, s);
     return hipGetLastError();
 }
 
