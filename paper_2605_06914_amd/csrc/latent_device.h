@@ -48,6 +48,10 @@ DEV unsigned lds_address(const void* p) { return (unsigned)(uintptr_t)(__attribu
 DEV void load_to_lds(const char* base, unsigned off, unsigned lds) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "m0", "memory");
 }
+// 64 lanes x 4 bytes likewise: what matters is that their lines are in the L2 afterwards.
+DEV void word_to_lds(const char* base, unsigned off, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds) : "m0", "memory");
+}
 #pragma clang diagnostic pop
 // All but this wave's N youngest loads have landed, its LDS accesses are done, and every wave of the workgroup is here.
 template <int N>

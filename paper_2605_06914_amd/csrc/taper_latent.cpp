@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <functional>
 #include <new>
 #include <string>
 #include <vector>
@@ -141,11 +142,82 @@ constexpr size_t kMostBlocks = (size_t)1 << 22;  // of a launch (which has fewer
 constexpr int kTile = taper::kLatentTileTokens, kRows = taper::kLatentTileRows;
 double tile_cost(int rows) { return rows <= 16 ? 1.0 : rows <= 32 ? 1.1 : 1.6; }
 constexpr double kItemCost = 1.5;  // of an item beside its tiles: its queries in, its partial rows out
-constexpr int kMostPieces = 64;    // of a segment: a row's pieces are merged by one wave
+constexpr int kMostPieces = 64;    // of a segment, about: a row's pieces are merged by some lanes of one workgroup
 
 struct Span {
     int seq0, page0, n_tokens, row0, n_rows;
 };
+
+// How spans are cut: into stretches that take `big` of a unit's equal share, and the last `small_share` of each into ones 1 / small_part
+// as long.  The long ones start first, and the short ones even out what is left.
+struct CutRule {
+    double big, small_share;
+    int small_part;
+};
+// (of these the one that ends soonest: the first two suit many spans of all lengths, the last few long ones)
+constexpr CutRule kCutRules[] = {{0.4, 0.0, 1}, {0.5, 0.3, 3}, {1.0, 0.4, 6}};
+constexpr int kXcds = 8;
+
+struct DecodeItems {
+    std::vector<taper_latent_item> items;
+    std::vector<int> list[kXcds];  // of each XCD, in the order in which its workgroups start
+    int64_t rows = 0;
+    double time = 0;  // when the last unit ends, in tiles
+};
+
+double item_cost(const taper_latent_item& it) { return (it.n_tokens + kTile - 1) / kTile * tile_cost(it.n_rows) + kItemCost; }
+
+void cut_spans(const std::vector<Span>& spans, int page_size, int units, double total, const CutRule& rule, DecodeItems* out) {
+    struct Unit {
+        double cost;
+        int first, n;
+    };
+    std::vector<Unit> stretches;
+    const double share = std::max(2.0 + kItemCost, total / units * rule.big);
+    for (const Span& s : spans) {
+        const int tiles = (s.n_tokens + kTile - 1) / kTile, least = std::max(1, tiles * 2 / kMostPieces);
+        const int big = std::max(least, (int)((share - kItemCost) / tile_cost(std::min(s.n_rows, kRows))));
+        int t = 0, n_small = 0;
+        if (tiles > big && rule.small_part > 1) n_small = std::max(std::max(least, big / rule.small_part), (int)(tiles * rule.small_share));
+        while (t < tiles) {
+            const int left = tiles - n_small - t;  // before the short ones
+            const int size = left > 0 ? big : std::max({least, big / rule.small_part, 2});
+            const int n = left > 0 ? (left + size - 1) / size : (tiles - t + size - 1) / size;  // equal stretches
+            const int t1 = t + ((left > 0 ? left : tiles - t) + n - 1) / n;
+            const int tok0 = t * kTile, tok1 = std::min(s.n_tokens, t1 * kTile);
+            // the row tiles of one stretch of tokens stay on one XCD, whose L2 then serves all but the first of them
+            Unit u = {0, (int)out->items.size(), 0};
+            for (int r = 0; r < s.n_rows; r += kRows) {
+                out->items.push_back({s.seq0, s.page0 + tok0 / page_size, tok1 - tok0, s.row0 + r, std::min(kRows, s.n_rows - r), (int32_t)(out->rows + r)});
+                u.cost += item_cost(out->items.back());
+                ++u.n;
+                if (u.cost > total / (2 * kXcds) || r + kRows >= s.n_rows) {
+                    stretches.push_back(u);
+                    u = {0, (int)out->items.size(), 0};
+                }
+            }
+            out->rows += s.n_rows;
+            t = t1;
+        }
+    }
+    std::stable_sort(stretches.begin(), stretches.end(), [](const Unit& x, const Unit& y) { return x.cost * y.n > y.cost * x.n; });
+    double load[kXcds] = {0};
+    for (const Unit& u : stretches) {
+        const int x = (int)(std::min_element(load, load + kXcds) - load);
+        load[x] += u.cost;
+        for (int i = 0; i < u.n; ++i) out->list[x].push_back(u.first + i);
+    }
+    std::vector<double> busy;
+    for (const auto& l : out->list) {
+        busy.assign(std::max(1, units / kXcds), 0.0);
+        for (int i : l) {
+            std::pop_heap(busy.begin(), busy.end(), std::greater<double>());
+            busy.back() += item_cost(out->items[i]);
+            std::push_heap(busy.begin(), busy.end(), std::greater<double>());
+        }
+        out->time = std::max(out->time, *std::max_element(busy.begin(), busy.end()));
+    }
+}
 
 void make_decode_items(const taper_latent_config& cfg, int units, taper_latent_plan* plan) {
     const taper::HostPlan& b = plan->batch;
@@ -162,95 +234,35 @@ void make_decode_items(const taper_latent_config& cfg, int units, taper_latent_p
                     plan->batch.tokens_unique += b.seg_len[k];
                 }
     }
-    auto row_tiles = [](const Span& s) { return (s.n_rows + kRows - 1) / kRows; };
-    auto span_tile_cost = [&](const Span& s) {
-        const int full = s.n_rows / kRows, rest = s.n_rows % kRows;
-        return full * tile_cost(kRows) + (rest ? tile_cost(rest) : 0.0);
-    };
     double total = 0;
-    for (const Span& s : spans) total += (s.n_tokens + kTile - 1) / kTile * span_tile_cost(s) + kItemCost * row_tiles(s);
-    // the largest item: an equal share of everything, or less where its granularity would leave units idle
-    double best_time = 1e300, best_most = 0;
-    std::vector<double> cost;
-    for (double f : {1.0, 0.7, 0.5, 0.35, 0.25}) {
-        const double most = std::max(1.0 + kItemCost, total / units * f);
-        cost.clear();
-        for (const Span& s : spans) {
-            const int tiles = (s.n_tokens + kTile - 1) / kTile;
-            const int per = std::max({1, (tiles + kMostPieces - 1) / kMostPieces, (int)((most - kItemCost) / tile_cost(std::min(s.n_rows, kRows)))});
-            const int n = (tiles + per - 1) / per;
-            const double each = (double)tiles / n * tile_cost(std::min(s.n_rows, kRows)) + kItemCost;
-            cost.insert(cost.end(), (size_t)n * row_tiles(s), each);
-        }
-        std::sort(cost.begin(), cost.end(), [](double x, double y) { return x > y; });
-        std::vector<double> load(units, 0.0);  // longest first onto the least loaded unit
-        auto later = [](double x, double y) { return x > y; };
-        for (double c : cost) {
-            std::pop_heap(load.begin(), load.end(), later);
-            load.back() += c;
-            std::push_heap(load.begin(), load.end(), later);
-        }
-        const double time = *std::max_element(load.begin(), load.end());
-        if (time < best_time * 0.97) {
-            best_time = time;
-            best_most = most;
-        }
-    }
-    // cut; the row tiles of one stretch of tokens stay on one XCD (workgroup i runs on XCD i mod 8), whose L2 then serves all but the
-    // first of them; each XCD gets its longest items first
-    struct Unit {
-        double cost;
-        int first, n;
-    };
-    std::vector<taper_latent_item> raw;
-    std::vector<Unit> stretches;
-    plan->piece_start.assign(b.n_seqs + 1, 0);
-    std::vector<std::pair<int, int32_t>> pieces;  // (sequence, partial row)
-    int64_t rows = 0;
     for (const Span& s : spans) {
-        const int tiles = (s.n_tokens + kTile - 1) / kTile;
-        const int per = std::max({1, (tiles + kMostPieces - 1) / kMostPieces, (int)((best_most - kItemCost) / tile_cost(std::min(s.n_rows, kRows)))});
-        const int n = (tiles + per - 1) / per;
-        for (int i = 0; i < n; ++i) {
-            const int t0 = (int)((int64_t)tiles * i / n), t1 = (int)((int64_t)tiles * (i + 1) / n);
-            const int tok0 = t0 * kTile, tok1 = std::min(s.n_tokens, t1 * kTile);
-            double in_unit = 0;
-            int first = (int)raw.size();
-            for (int r = 0; r < s.n_rows; r += kRows) {
-                const int nr = std::min(kRows, s.n_rows - r);
-                raw.push_back({s.seq0, s.page0 + tok0 / cfg.page_size, tok1 - tok0, s.row0 + r, nr, (int32_t)(rows + r)});
-                in_unit += (t1 - t0) * tile_cost(nr) + kItemCost;
-                if (in_unit > total / 16) {
-                    stretches.push_back({in_unit, first, (int)raw.size() - first});
-                    first = (int)raw.size();
-                    in_unit = 0;
-                }
-            }
-            if ((int)raw.size() > first) stretches.push_back({in_unit, first, (int)raw.size() - first});
-            for (int q = s.seq0; q < s.seq0 + s.n_rows / H; ++q) pieces.push_back({q, (int32_t)(rows + (int64_t)(q - s.seq0) * H)});
-            rows += s.n_rows;
-        }
+        const int full = s.n_rows / kRows, rest = s.n_rows % kRows;
+        const double each = full * tile_cost(kRows) + (rest ? tile_cost(rest) : 0.0);
+        total += (s.n_tokens + kTile - 1) / kTile * each + kItemCost * (full + (rest > 0));
     }
-    plan->n_partial_rows = rows;
-    std::stable_sort(pieces.begin(), pieces.end(), [](const std::pair<int, int32_t>& x, const std::pair<int, int32_t>& y) { return x.first < y.first; });
-    for (const auto& p : pieces) {
-        plan->piece_start[p.first + 1]++;
-        plan->piece_row.push_back(p.second);
+    DecodeItems best;
+    for (const CutRule& rule : kCutRules) {
+        DecodeItems d;
+        cut_spans(spans, cfg.page_size, units, total, rule, &d);
+        if (best.items.empty() || d.time < 0.98 * best.time) std::swap(best, d);
     }
+    // the pieces of each sequence's rows: one for every stretch that holds tokens of it
+    plan->n_partial_rows = best.rows;
+    plan->piece_start.assign(b.n_seqs + 1, 0);
+    auto each_piece = [&](auto f) {
+        for (const taper_latent_item& it : best.items)
+            for (int q = (it.row0 + H - 1) / H; q * H < it.row0 + it.n_rows; ++q) f(q, it.part_row + q * H - it.row0);  // the item with head 0's row
+    };
+    each_piece([&](int q, int) { plan->piece_start[q + 1]++; });
     for (int s = 0; s < b.n_seqs; ++s) plan->piece_start[s + 1] += plan->piece_start[s];
-    std::stable_sort(stretches.begin(), stretches.end(), [](const Unit& x, const Unit& y) { return x.cost / x.n > y.cost / y.n; });
-    constexpr int kXcds = 8;
-    double load[kXcds] = {0};
-    std::vector<int> list[kXcds];
-    for (const Unit& u : stretches) {
-        const int x = (int)(std::min_element(load, load + kXcds) - load);
-        load[x] += u.cost;
-        for (int i = 0; i < u.n; ++i) list[x].push_back(u.first + i);
-    }
+    plan->piece_row.resize(plan->piece_start[b.n_seqs]);
+    std::vector<int32_t> at(plan->piece_start.begin(), plan->piece_start.end() - 1);
+    each_piece([&](int q, int row) { plan->piece_row[at[q]++] = row; });
+    // workgroup i runs on XCD i mod 8
     size_t longest = 0;
-    for (const auto& l : list) longest = std::max(longest, l.size());
+    for (const auto& l : best.list) longest = std::max(longest, l.size());
     for (size_t i = 0; i < longest; ++i)
-        for (int x = 0; x < kXcds; ++x) plan->items.push_back(i < list[x].size() ? raw[list[x][i]] : taper_latent_item{0, 0, 0, 0, 0, 0});
+        for (int x = 0; x < kXcds; ++x) plan->items.push_back(i < best.list[x].size() ? best.items[best.list[x][i]] : taper_latent_item{0, 0, 0, 0, 0, 0});
 }
 
 int build_decode(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, int stride, const int32_t* group, const int32_t* prefix,

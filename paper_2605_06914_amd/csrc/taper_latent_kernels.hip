@@ -5,6 +5,7 @@
 // softmax(scale q_lat . (c, r)) . c for items of up to 64 query rows and some tokens, as partial rows.  finish_kernel merges
 // a row's partials through their (max, sum) and applies W_v[h].
 #include <cmath>
+#include <type_traits>
 
 #include "latent_device.h"
 
@@ -94,16 +95,15 @@ struct DecodeSmem {
     f32x4 mx[kLatentTileRows];   // a row's maximum in each of the four pages
     f32x4 sum[kLatentTileRows];
     bf16x8 q_rope[4][2][64];     // [row tile][k-step][lane]: the queries' rotated parts (the rest is in registers, which these would not fit)
+    unsigned sink[64];           // nobody reads it (see touch)
     __bf16 tile[2][4][(R + kRopeDim) * 16];
 };
 
-template <int R>
-DEV void fetch_half_page(const char* pages, int page, const __bf16* to, int half, int lane) {
-    constexpr int BYTES = (R + kRopeDim) * 32;
-    const char* base = pages + (int64_t)uniform(page) * BYTES + half * (BYTES / 2);
-    const unsigned lds = uniform(lds_address(to)) + half * (BYTES / 2);
-#pragma unroll
-    for (int i = 0; i < BYTES / 2048; ++i) load_to_lds(base + i * 1024, lane * 16, lds + i * 1024);  // (scalar sums: one lane offset for all)
+// Where P lies in a tile: the rotated parts of pages 2i and 2i + 1 hold row tiles 0, 1 and 2, 3 of both, a lane's 4 tokens of each
+// page side by side as the value product takes them.
+template <int KD16>
+DEV bf16x4* weights_at(const __bf16* tile, int page, int k, int lane) {
+    return (bf16x4*)(tile + ((page & ~1) + (k >> 1)) * KD16 + (KD16 - kRopeDim * 16)) + ((k & 1) * 64 + lane) * 2 + (page & 1);
 }
 
 template <int R, int NT>  // NT row tiles of 16
@@ -116,9 +116,25 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
     const int last_page = (it.n_tokens + 15) / 16 - 1, n_tiles = (it.n_tokens + 63) / 64;
     const char* pages = (const char*)a.pages;
     const float c = sh.scale_log2e;
+    constexpr int LOADS = (R + kRopeDim) / 64;  // a wave brings half of its page, a KiB at a time
+    const unsigned half_bytes = (wave >> 2) * (R + kRopeDim) * 16;
 
-    fetch_half_page<R>(pages, row[min(pg, last_page)], sm.tile[0][pg], wave >> 2, lane);
-    int next = row[min(4 + pg, last_page)];
+    auto page = [&](int t) { return pages + (int64_t)row[min(4 * t + pg, last_page)] * ((R + kRopeDim) * 32) + half_bytes; };  // (past the end: the last one)
+    // Brings a tile's lines into the L2 two tiles before its own loads: pages are scattered, and from memory a tile took longer than
+    // another tile's work (one tile ahead only, a tile of 64 rows took 8400 clocks, of which 3000 were waiting).
+    constexpr int LINES = (R + kRopeDim) / 8, TOUCHES = (LINES + 63) / 64;
+    auto touch = [&](const char* from) {
+#pragma unroll
+        for (int i = 0; i < TOUCHES; ++i) word_to_lds(from, min(64 * i + lane, LINES - 1) * 128, uniform(lds_address(sm.sink)));
+    };
+    {
+        const char* from = page(0);
+        const unsigned to = uniform(lds_address(sm.tile[0][pg])) + half_bytes;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load_to_lds(from + i * 1024, lane * 16, to + i * 1024);  // (scalar sums: one lane offset for all)
+    }
+    const char *next = page(1), *next2 = page(2);
+    touch(next2);
     bf16x8 qf[NS][JL];
 #pragma unroll
     for (int k = 0; k < NS; ++k) {
@@ -140,53 +156,60 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
     }
 #pragma unroll
     for (int k = 0; k < NS; ++k) l[k] = 0.f;
-    for (int t = 0; t < n_tiles; ++t) {
-        wait_loads_and_meet<0>();  // tile t is here for all, and all are done with tile t - 1
-        if (t + 1 < n_tiles) {
-            fetch_half_page<R>(pages, next, sm.tile[(t + 1) & 1][pg], wave >> 2, lane);
-            next = row[min(4 * (t + 2) + pg, last_page)];
-        }
+    auto step = [&](const int t, auto last) {
+        wait_loads_and_meet<TOUCHES>();  // tile t is here for all, and all are done with tile t - 1
+        const char* const from = next;
+        const unsigned to = uniform(lds_address(sm.tile[(t + 1) & 1][pg])) + half_bytes;
+        next = next2;
+        next2 = page(t + 3);
+        auto load = [&](int i) {  // (between other instructions: all at once they would hold up what follows)
+            if (!last && i < LOADS) load_to_lds(from + i * 1024, lane * 16, to + i * 1024);
+        };
         __bf16* const mine = sm.tile[t & 1][pg];
         const int valid = it.n_tokens - 64 * t - 16 * pg;  // of this wave's page
-        if (it.n_tokens - 64 * t < 64) {  // what follows the last token may be anything: zeros, so that its zero weight meets no NaN
+        if (last && it.n_tokens - 64 * t < 64) {  // what follows the last token may be anything: zeros, so that its zero weight meets no NaN
             for (int i = lane + (wave >> 2) * 64; i < KD / 8 * 16; i += 128)
                 if ((i & 15) >= valid) *(u32x4*)(mine + i * 8) = u32x4{0, 0, 0, 0};
             meet();
         }
         f32x4 s[NS];
         if (scores) {
+            constexpr int AHEAD = 4, JK = JL + 2;
+            bf16x8 kf[AHEAD];
+            const __bf16* const k_at = mine + g * 128 + n * 8;
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) kf[j] = *(const bf16x8*)(k_at + j * 512);
 #pragma unroll
             for (int k = 0; k < NS; ++k) s[k] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < JL; ++j) {
-                const bf16x8 kf = *(const bf16x8*)(mine + (4 * j + g) * 128 + n * 8);
+            for (int j = 0; j < JK; ++j) {
 #pragma unroll
-                for (int k = 0; k < NS; ++k) s[k] = mfma16(kf, qf[k][j], s[k]);
-                if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (else the whole page is read ahead, into registers that are not there)
+                for (int k = 0; k < NS; ++k) s[k] = mfma16(kf[j % AHEAD], j < JL ? qf[k][j] : sm.q_rope[k0 + k][j - JL][lane], s[k]);
+                if (j + AHEAD < JK) kf[j % AHEAD] = *(const bf16x8*)(k_at + (j + AHEAD) * 512);
+                if (j % 2 == 1) load(j / 2);
+                __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const bf16x8 kf = *(const bf16x8*)(mine + (R / 8 + 4 * j + g) * 128 + n * 8);
-#pragma unroll
-                for (int k = 0; k < NS; ++k) s[k] = mfma16(kf, sm.q_rope[k0 + k][j][lane], s[k]);
-            }
+            for (int i = JK / 2; i < LOADS; ++i) load(i);
 #pragma unroll
             for (int k = 0; k < NS; ++k) {
-                if (valid < 16)
+                if (last && valid < 16)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[k][i] = 4 * g + i < valid ? s[k][i] : -INFINITY;
                 const float mx = max_lane_groups(max4(s[k]));
                 if (g == 0) ((float*)&sm.mx[16 * (k0 + k) + n])[pg] = mx;
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) load(i);
         }
+        if (!last) touch(next2);
         meet();
         float alpha[NT];
         bool higher = false;
 #pragma unroll
         for (int k = 0; k < NT; ++k) {
-            const f32x4 of = sm.mx[16 * k + n];
-            const float mx = max4(of);
-            const float mn = max2(m[k], mx * c);
+            const float mn = max2(m[k], max4(sm.mx[16 * k + n]) * c);
             higher |= mn > m[k];
             alpha[k] = fast_exp2(m[k] - mn);
             m[k] = mn;
@@ -199,7 +222,8 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
 #pragma unroll
                 for (int i = 0; i < 4; ++i) p[i] = fast_exp2(fmaf(s[k][i], c, -mk));
                 l[k] = fmaf(l[k], NT == NS || wave < 4 ? alpha[k] : alpha[NT - NS + k], (p[0] + p[1]) + (p[2] + p[3]));
-                ((bf16x4*)(mine + R * 16))[(k0 + k) * 64 + lane] = __builtin_convertvector(p, bf16x4);  // (weights of at most 1, in 8 bits each)
+                // (weights of at most 1, in 8 bits each); 8 tokens of a lane from two pages lie together
+                *weights_at<KD * 16>(sm.tile[t & 1][0], pg, k0 + k, lane) = __builtin_convertvector(p, bf16x4);
             }
         }
         if (__any(higher)) {
@@ -209,32 +233,35 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
                 for (int d = 0; d < DT; ++d) O[k][d] *= alpha[k];
         }
         meet();
+        const __bf16* const v_at = sm.tile[t & 1][0] + wave * DT * 256 + (lane >> 1 & 1) * 128 + (4 * g + (n >> 2)) * 8 + (lane & 1) * 4;
+        auto columns = [&](int x) {  // 16 columns of 32 tokens; x: column group, then pair of pages
+            typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+            const __bf16* at = v_at + x / DT * 2 * (KD * 16) + x % DT * 256;
+            const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)at), v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + KD * 16));
+            return cat(__builtin_bit_cast(bf16x4, v0), __builtin_bit_cast(bf16x4, v1));
+        };
+        bf16x8 pf[NT], vf[2] = {columns(0), columns(1)};
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            bf16x8 pf[NT];
+        for (int x = 0; x < 2 * DT; ++x) {
+            if (x % DT == 0)
 #pragma unroll
-            for (int k = 0; k < NT; ++k)
-                pf[k] = cat(((const bf16x4*)(sm.tile[t & 1][2 * ks] + R * 16))[k * 64 + lane], ((const bf16x4*)(sm.tile[t & 1][2 * ks + 1] + R * 16))[k * 64 + lane]);
+                for (int k = 0; k < NT; ++k) pf[k] = *(const bf16x8*)weights_at<KD * 16>(sm.tile[t & 1][0], x / DT * 2, k, lane);
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const int at = (wave * DT + d) * 256 + (lane >> 1 & 1) * 128 + (4 * g + (n >> 2)) * 8 + (lane & 1) * 4;
-                typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
-                const bf16x4 v0 = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(sm.tile[t & 1][2 * ks] + at)));
-                const bf16x4 v1 = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(sm.tile[t & 1][2 * ks + 1] + at)));
-                const bf16x8 vf = cat(v0, v1);
-#pragma unroll
-                for (int k = 0; k < NT; ++k) O[k][d] = mfma16(vf, pf[k], O[k][d]);
-            }
+            for (int k = 0; k < NT; ++k) O[k][x % DT] = mfma16(vf[x % 2], pf[k], O[k][x % DT]);
+            if (x + 2 < 2 * DT) vf[x % 2] = columns(x + 2);
+            __builtin_amdgcn_sched_barrier(0);
         }
-    }
-    // a row's sum: over the lane groups, and over the waves' pages
+    };
+    for (int t = 0; t < n_tiles - 1; ++t) step(t, std::false_type());
+    step(n_tiles - 1, std::true_type());
+    // a row's sum: over the lane groups, and over the waves' pages (and nothing in flight to LDS when the workgroup ends)
     if (scores)
 #pragma unroll
         for (int k = 0; k < NS; ++k) {
             const float mine = sum_lane_groups(l[k]);
             if (g == 0) ((float*)&sm.sum[16 * (k0 + k) + n])[pg] = mine;
         }
-    meet();
+    wait_loads_and_meet<0>();
 #pragma unroll
     for (int k = 0; k < NT; ++k) {
         const int r = 16 * k + n;
