@@ -77,10 +77,9 @@ __global__ __launch_bounds__(64) void absorb_kernel(const LatentShape sh, const 
 // The attention.  A workgroup of 8 waves holds up to 64 query rows and takes 64 tokens (4 pages) at a time through LDS.  For the
 // scores, S^T = C Q^T, a wave owns a page and half of the rows (its queries stay in registers: 32 rows x 576 values are 144 of
 // them); for the product with the values, O^T = C^T P^T, it owns R / 8 of their columns and all rows.  K and V are the same
-// bytes, and LDS delivers them twice and once to the workgroup instead of once to each wave.  What the waves exchange is the rows'
-// maxima and P (bf16, in the layout in which the score product leaves it and the value product wants it; it takes the place of the
-// page's rotated parts, which are of no more use then).  V's operand is columns
-// of a token-major page: ds_read_b64_tr_b16 reads 4 tokens x 16 columns transposed.
+// bytes, and LDS delivers them twice and once to the workgroup instead of once to each wave.  What the waves exchange is P (bf16, in
+// the layout in which the score product leaves it and the value product wants it).  V's operand is columns of a token-major page:
+// ds_read_b64_tr_b16 reads 4 tokens x 16 columns transposed.
 // ---------------------------------------------------------------------------
 constexpr int kDecodeWaves = 8;
 // A partial row travels divided by its own sum, in half precision after division by a power of two of each wave's R / 8 columns that
@@ -94,21 +93,20 @@ struct DecodeSmem {
     // (the small ones first: an LDS access has 16 bits of offset, and addresses beyond it cost a register each)
     f32x4 mx[kLatentTileRows];   // a row's maximum in each of the four pages
     f32x4 sum[kLatentTileRows];
-    bf16x8 q_rope[4][2][64];     // [row tile][k-step][lane]: the queries' rotated parts (the rest is in registers, which these would not fit)
+    bf16x8 p[2][4][64];          // [pair of pages][row tile][lane]: a lane's 4 tokens of each page side by side, as the value product takes them
+    int higher[kDecodeWaves];    // whether a wave's scores need a new reference
     unsigned sink[64];           // nobody reads it (see touch)
     __bf16 tile[2][4][(R + kRopeDim) * 16];
 };
 
-// Where P lies in a tile: the rotated parts of pages 2i and 2i + 1 hold row tiles 0, 1 and 2, 3 of both, a lane's 4 tokens of each
-// page side by side as the value product takes them.
-template <int KD16>
-DEV bf16x4* weights_at(const __bf16* tile, int page, int k, int lane) {
-    return (bf16x4*)(tile + ((page & ~1) + (k >> 1)) * KD16 + (KD16 - kRopeDim * 16)) + ((k & 1) * 64 + lane) * 2 + (page & 1);
-}
-
+// Weights are taken relative to a row's reference, the largest score of some earlier tile: waves that own different pages of a row can
+// then weigh their scores at once and meet once a tile, instead of meeting for each tile's maximum first.  A score that is more than
+// this above its reference (in log2; a first tile always is) makes all waves meet for new references and weigh the tile again.  Weights
+// are then at most 2^6: a bf16 weight has 8 bits whatever its size, sums and accumulators are fp32.
+constexpr float kMostAbove = 6.f;
 template <int R, int NT>  // NT row tiles of 16
 DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const taper_latent_item& it, DecodeSmem<R>& sm) {
-    constexpr int KD = R + kRopeDim, JL = R / 32, DT = R / 16 / kDecodeWaves, NS = (NT + 1) / 2;  // NS: row tiles of a wave's scores
+    constexpr int KD = R + kRopeDim, JK = KD / 32, DT = R / 16 / kDecodeWaves, NS = (NT + 1) / 2;  // NS: row tiles of a wave's scores
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     const int pg = wave & 3, k0 = (wave >> 2) * NS;  // page and first row tile of this wave's scores
     const bool scores = k0 < NT;
@@ -135,16 +133,12 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
     }
     const char *next = page(1), *next2 = page(2);
     touch(next2);
-    bf16x8 qf[NS][JL];
+    bf16x8 qf[NS][JK];
 #pragma unroll
     for (int k = 0; k < NS; ++k) {
         const __bf16* q = (const __bf16*)a.q_lat + (int64_t)(it.row0 + min(16 * (k0 + k) + n, it.n_rows - 1)) * KD + 8 * g;
 #pragma unroll
-        for (int j = 0; j < JL; ++j) qf[k][j] = *(const bf16x8*)(q + 32 * j);
-        if (pg == 0 && scores) {
-            sm.q_rope[k0 + k][0][lane] = *(const bf16x8*)(q + R);
-            sm.q_rope[k0 + k][1][lane] = *(const bf16x8*)(q + R + 32);
-        }
+        for (int j = 0; j < JK; ++j) qf[k][j] = *(const bf16x8*)(q + 32 * j);
     }
     f32x4 O[NT][DT];
     float m[NT], l[NS];  // running maxima of all rows; sums of this wave's page and rows
@@ -173,8 +167,22 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
             meet();
         }
         f32x4 s[NS];
+        float sum[NS];
+        bool higher = false;
+        auto ref = [&](int k) { return NT == NS || wave < 4 ? m[k] : m[NT - NS + k]; };  // reference of this wave's rows
+        auto weigh = [&] {
+#pragma unroll
+            for (int k = 0; k < NS; ++k) {
+                f32x4 p;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[i] = fast_exp2(fmaf(s[k][i], c, -ref(k)));
+                sum[k] = (p[0] + p[1]) + (p[2] + p[3]);
+                // (8 bits of each weight, whatever its size); 8 tokens of a lane from two pages lie together
+                ((bf16x4*)&sm.p[pg >> 1][k0 + k][lane])[pg & 1] = __builtin_convertvector(p, bf16x4);
+            }
+        };
         if (scores) {
-            constexpr int AHEAD = 4, JK = JL + 2;
+            constexpr int AHEAD = 3;
             bf16x8 kf[AHEAD];
             const __bf16* const k_at = mine + g * 128 + n * 8;
 #pragma unroll
@@ -184,7 +192,7 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
 #pragma unroll
             for (int j = 0; j < JK; ++j) {
 #pragma unroll
-                for (int k = 0; k < NS; ++k) s[k] = mfma16(kf[j % AHEAD], j < JL ? qf[k][j] : sm.q_rope[k0 + k][j - JL][lane], s[k]);
+                for (int k = 0; k < NS; ++k) s[k] = mfma16(kf[j % AHEAD], qf[k][j], s[k]);
                 if (j + AHEAD < JK) kf[j % AHEAD] = *(const bf16x8*)(k_at + (j + AHEAD) * 512);
                 if (j % 2 == 1) load(j / 2);
                 __builtin_amdgcn_sched_barrier(0);
@@ -197,42 +205,42 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[k][i] = 4 * g + i < valid ? s[k][i] : -INFINITY;
                 const float mx = max_lane_groups(max4(s[k]));
+                higher |= !(mx * c <= ref(k) + kMostAbove);
                 if (g == 0) ((float*)&sm.mx[16 * (k0 + k) + n])[pg] = mx;
             }
+            weigh();
         } else {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) load(i);
         }
         if (!last) touch(next2);
+        if (lane == 0) sm.higher[wave] = 0;
+        if (__any(higher) && lane == 0) sm.higher[wave] = 1;
         meet();
-        float alpha[NT];
-        bool higher = false;
+        {
+            typedef int i32x4 __attribute__((ext_vector_type(4)));
+            const i32x4 x = ((const i32x4*)sm.higher)[0] | ((const i32x4*)sm.higher)[1];
+            if (uniform(x[0] | x[1] | x[2] | x[3])) {  // (all waves alike)
+                float alpha[NT];
 #pragma unroll
-        for (int k = 0; k < NT; ++k) {
-            const float mn = max2(m[k], max4(sm.mx[16 * k + n]) * c);
-            higher |= mn > m[k];
-            alpha[k] = fast_exp2(m[k] - mn);
-            m[k] = mn;
-        }
-        if (scores) {
+                for (int k = 0; k < NT; ++k) {
+                    const float mn = max2(m[k], max4(sm.mx[16 * k + n]) * c);
+                    alpha[k] = fast_exp2(m[k] - mn);
+                    m[k] = mn;
 #pragma unroll
-            for (int k = 0; k < NS; ++k) {
-                const float mk = NT == NS || wave < 4 ? m[k] : m[NT - NS + k];
-                f32x4 p;
+                    for (int d = 0; d < DT; ++d) O[k][d] *= alpha[k];
+                }
+                if (scores) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = fast_exp2(fmaf(s[k][i], c, -mk));
-                l[k] = fmaf(l[k], NT == NS || wave < 4 ? alpha[k] : alpha[NT - NS + k], (p[0] + p[1]) + (p[2] + p[3]));
-                // (weights of at most 1, in 8 bits each); 8 tokens of a lane from two pages lie together
-                *weights_at<KD * 16>(sm.tile[t & 1][0], pg, k0 + k, lane) = __builtin_convertvector(p, bf16x4);
+                    for (int k = 0; k < NS; ++k) l[k] *= NT == NS || wave < 4 ? alpha[k] : alpha[NT - NS + k];
+                    weigh();
+                }
+                meet();
             }
         }
-        if (__any(higher)) {
+        if (scores)
 #pragma unroll
-            for (int k = 0; k < NT; ++k)
-#pragma unroll
-                for (int d = 0; d < DT; ++d) O[k][d] *= alpha[k];
-        }
-        meet();
+            for (int k = 0; k < NS; ++k) l[k] += sum[k];
         const __bf16* const v_at = sm.tile[t & 1][0] + wave * DT * 256 + (lane >> 1 & 1) * 128 + (4 * g + (n >> 2)) * 8 + (lane & 1) * 4;
         auto columns = [&](int x) {  // 16 columns of 32 tokens; x: column group, then pair of pages
             typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
@@ -245,7 +253,7 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
         for (int x = 0; x < 2 * DT; ++x) {
             if (x % DT == 0)
 #pragma unroll
-                for (int k = 0; k < NT; ++k) pf[k] = *(const bf16x8*)weights_at<KD * 16>(sm.tile[t & 1][0], x / DT * 2, k, lane);
+                for (int k = 0; k < NT; ++k) pf[k] = sm.p[x / DT][k][lane];
 #pragma unroll
             for (int k = 0; k < NT; ++k) O[k][x % DT] = mfma16(vf[x % 2], pf[k], O[k][x % DT]);
             if (x + 2 < 2 * DT) vf[x % 2] = columns(x + 2);
