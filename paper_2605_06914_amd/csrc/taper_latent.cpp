@@ -137,11 +137,11 @@ int upload(taper_latent_plan* plan, const Layout& lay, size_t image, hipStream_t
 constexpr size_t kMostBlocks = (size_t)1 << 22;  // of a launch (which has fewer than 2^32 threads)
 
 // ---------------------------------------------------------------------------- decode plan
-// What some tokens cost: their tiles, at the price of the rows they meet (a tile of up to 32 rows is bound by its bytes, one of
-// 64 by its products).
+// What some tokens cost: their tiles, at the price of the rows they meet (measured: a tile of 16 rows takes 3.1 us when all units
+// stream from memory, one of 64 rows 2.6 us where the L2 has it, a little more than the former where it has not).
 constexpr int kTile = taper::kLatentTileTokens, kRows = taper::kLatentTileRows;
-double tile_cost(int rows) { return rows <= 16 ? 1.0 : rows <= 32 ? 1.1 : 1.6; }
-constexpr double kItemCost = 1.5;  // of an item beside its tiles: its queries in, its partial rows out
+double tile_cost(int rows) { return rows <= 16 ? 0.9 : rows <= 32 ? 0.95 : 1.1; }
+constexpr double kItemCost = 3.0;  // of an item beside its tiles: its queries in, its partial rows out
 constexpr int kMostPieces = 64;    // of a segment, about: a row's pieces are merged by some lanes of one workgroup
 
 struct Span {
@@ -154,8 +154,9 @@ struct CutRule {
     double big, small_share;
     int small_part;
 };
-// (of these the one that ends soonest: the first two suit many spans of all lengths, the last few long ones)
-constexpr CutRule kCutRules[] = {{0.4, 0.0, 1}, {0.5, 0.3, 3}, {1.0, 0.4, 6}};
+// (of these the one that ends soonest: the first suits short spans, an item a unit, the second spans of all lengths, the others few
+// long ones)
+constexpr CutRule kCutRules[] = {{1.2, 0.0, 1}, {0.4, 0.0, 1}, {0.5, 0.3, 3}, {1.0, 0.4, 6}};
 constexpr int kXcds = 8;
 
 struct DecodeItems {

@@ -315,7 +315,7 @@ __global__ __launch_bounds__(512, 2) void latent_decode_kernel(const LatentShape
 // ---------------------------------------------------------------------------
 template <int R, int HD, int SB>
 __global__ __launch_bounds__(512) void finish_kernel(const LatentShape sh, const LatentDecodeArgs a) {
-    constexpr int PITCH = R + 8, PER = R * SB / 512, UN = 4;  // PER: columns of a thread; UN: pieces in flight
+    constexpr int PITCH = R + 8, PER = R * SB / 512, UN = SB == 4 ? 8 : 4;  // PER: columns of a thread; UN: pieces in flight
     typedef _Float16 part_t __attribute__((ext_vector_type(PER)));
     __shared__ __align__(16) __bf16 o[2][SB][PITCH];
     __shared__ float dots[SB][2], norm[SB];
@@ -328,37 +328,48 @@ __global__ __launch_bounds__(512) void finish_kernel(const LatentShape sh, const
 #pragma unroll
         for (int j = 0; j < R / 32; ++j) wf[j] = *(const bf16x8*)(w + 32 * j);
     {
-        const int i = tid / (512 / SB), d0 = tid % (512 / SB) * PER, s = s0 + i, chunk = d0 / (R / kDecodeWaves);
-        float acc[PER];
+        constexpr int THREADS = 512 / SB, LANES = THREADS < 64 ? THREADS : 64;
+        const int i = tid / THREADS, d0 = tid % THREADS * PER, s = s0 + i, chunk = d0 / (R / kDecodeWaves);
+        float acc[PER], M = -INFINITY, L = 0.f;
 #pragma unroll
         for (int j = 0; j < PER; ++j) acc[j] = 0.f;
-        if (s < a.n_seqs) {
-            const int b = a.piece_start[s], e = a.piece_start[s + 1];
-            float M = -INFINITY, L = 0.f;
-            for (int p = b; p < e; p += UN) {
+        const int b = s < a.n_seqs ? a.piece_start[s] : 0, e = s < a.n_seqs ? a.piece_start[s + 1] : 0;
+        // 32 pieces at a time: a lane finds one's row and statistics, all of them their common maximum; the rows follow, some in flight
+        for (int p0 = b; p0 < e; p0 += 32) {
+            const int here = min(32, e - p0), mine = min(lane & 31, here - 1);
+            const int r = a.piece_row[p0 + mine] + h;
+            const float2 ml = *(const float2*)&a.stats[r];
+            float most = ml.x;
 #pragma unroll
-                for (int u = 0; u < UN; ++u) M = fmaxf(M, a.stats[a.piece_row[min(p + u, e - 1)] + h].m);
-            }
-            for (int p = b; p < e; p += UN) {
+            for (int x = 16; x; x >>= 1) most = fmaxf(most, __shfl_xor(most, x, 32));
+            most = fmaxf(most, M);
+            const float old = fast_exp2(M - most), w = (lane & 31) < here ? ml.y * fast_exp2(ml.x - most) : 0.f;
+            float total = w;
+#pragma unroll
+            for (int x = 16; x; x >>= 1) total += __shfl_xor(total, x, 32);
+            L = fmaf(L, old, total);
+            M = most;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) acc[j] *= old;
+            for (int p = 0; p < here; p += UN) {
                 part_t v[UN];
-                float2 ml[UN];
                 int ex[UN];
 #pragma unroll
                 for (int u = 0; u < UN; ++u) {
-                    const int64_t r = a.piece_row[min(p + u, e - 1)] + h;
-                    ml[u] = *(const float2*)&a.stats[r];
-                    ex[u] = a.stats[r].exponent[chunk];
-                    v[u] = *(const part_t*)((const _Float16*)a.part + r * R + d0);
+                    const int64_t at = __shfl(r, min(p + u, here - 1), 32);
+                    ex[u] = a.stats[at].exponent[chunk];
+                    v[u] = *(const part_t*)((const _Float16*)a.part + at * R + d0);
                 }
 #pragma unroll
                 for (int u = 0; u < UN; ++u) {
-                    const float wt = p + u < e ? ml[u].y * fast_exp2(ml[u].x - M) : 0.f;
-                    L += wt;
-                    const float up = wt * __uint_as_float((unsigned)(127 + ex[u]) << 23);
+                    const float up = __shfl(w, min(p + u, here - 1), 32) * __uint_as_float((unsigned)(127 + ex[u]) << 23);
+                    if (p + u < here)
 #pragma unroll
-                    for (int j = 0; j < PER; ++j) acc[j] = p + u < e ? fmaf(up, (float)v[u][j], acc[j]) : acc[j];
+                        for (int j = 0; j < PER; ++j) acc[j] = fmaf(up, (float)v[u][j], acc[j]);
                 }
             }
+        }
+        if (s < a.n_seqs) {
             const float inv = 1.0f / L;
 #pragma unroll
             for (int j = 0; j < PER; ++j) acc[j] *= inv;
@@ -369,10 +380,9 @@ __global__ __launch_bounds__(512) void finish_kernel(const LatentShape sh, const
                 float dot = 0.f;
 #pragma unroll
                 for (int j = 0; j < PER; ++j) dot = fmaf((float)rest[j], acc[j], dot);
-                constexpr int LANES = 512 / SB < 64 ? 512 / SB : 64;
 #pragma unroll
                 for (int x = LANES / 2; x; x >>= 1) dot += __shfl_xor(dot, x);
-                if (lane % LANES == 0) dots[i][tid % (512 / SB) / 64] = dot;
+                if (lane % LANES == 0) dots[i][tid % THREADS / 64] = dot;
                 if (d0 == 0) norm[i] = M + log2f(L);
             }
         }
@@ -435,7 +445,7 @@ static void launch_finish(bool many, const LatentShape& sh, const LatentDecodeAr
 }
 
 hipError_t launch_latent_decode(const LatentShape& sh, const LatentDecodeArgs& a, hipStream_t s) {
-    const int s_per_block = 64;
+    const int s_per_block = a.n_seqs <= 256 ? 16 : 64;  // (W is read again for each block of sequences; few sequences leave little else to do at once)
     const dim3 grid(sh.n_heads, sh.latent_dim / 128, (a.n_seqs + s_per_block - 1) / s_per_block);
     if (sh.head_dim == 128) hipLaunchKernelGGL((absorb_kernel<4>), grid, dim3(64), 0, s, sh, a, s_per_block);
     else hipLaunchKernelGGL((absorb_kernel<2>), grid, dim3(64), 0, s, sh, a, s_per_block);
