@@ -40,6 +40,12 @@ DEV float sum_lane_groups(float v) {
     return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
+// The power of two that brings the largest magnitude `most` into [0.5, 1) when divided by it; 2^e and 2^-e are normal numbers.
+DEV int exponent_of(float most) {
+    const int e = (int)((__float_as_uint(most) >> 23) & 0xff) - 126;
+    return e < -126 ? -126 : (e > 126 ? 126 : e);
+}
+
 DEV unsigned lds_address(const void* p) { return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
 // 64 lanes x 16 bytes: lane l's from base + off (per lane) to LDS address `lds` + 16 l.  The statement itself keeps the wait
 // states between a vector instruction's write of the base and the load (the compiler does not look inside).

@@ -44,8 +44,8 @@ struct PromptTile {
     int32_t row0, n_rows;        // rows of q
     int32_t first_pos;           // position of the first row's token in its sequence
     int32_t prefix_len;          // tokens of the shared prefix
-    int32_t prefix_e, suffix_e;  // expanded pages of the prefix and of the private tokens begin here
-    int32_t page_begin, page_end;  // the pages of the sequence (prefix pages, then private ones) this tile's item meets
+    int32_t prefix_e, suffix_e;  // expanded pages of the prefix and of the private tokens begin here (even numbers)
+    int32_t page_begin, page_end;  // the pages (of the prefix, an even number, then private ones) this tile's item meets; page_begin is even
     int32_t part_row;            // partial rows of head 0, or -1: the item is its rows' only one and writes the result
     int32_t n_pieces;            // items of the same rows; their partial rows are n_rows apart
 };
@@ -54,7 +54,8 @@ struct PromptArgs {
     const int32_t* e_valid;      // [n_expanded] tokens of it that exist
     const PromptTile* tiles;     // [n_tiles], longest first
     const PromptTile* merges;    // [n_merges] row tiles whose keys are cut into pieces
-    void* kv;                    // bf16 [head of the group][n_expanded][K | V], tiles as in the pool of taper_attn.h
+    void* kv;                    // [head of the group][n_expanded / 2][K, K, V of a pair of pages] (see the kernels)
+    int32_t* format;             // [head of the group][n_chunks][keys, values]: 1 where four pages are bf16 instead of half precision
     float2* ml;
     float* part;                 // [head][partial rows][head_dim]
     const void* q;
@@ -62,6 +63,7 @@ struct PromptArgs {
     const void* pages;
     void* out;
     float* lse;
+    int32_t n_chunks, units;     // fours of expanded pages; compute units
     int32_t n_expanded, n_tiles, n_merges, n_partial_rows;  // partial rows of one head
     int32_t heads_at_once;
 };

@@ -315,8 +315,8 @@ int build_decode(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, 
 }
 
 // ---------------------------------------------------------------------------- prompt plan
-constexpr int kPromptRows = 128;
-constexpr int64_t kMostExpandedBytes = (int64_t)1 << 30;  // of the heads expanded at a time
+constexpr int kPromptRows = 256;
+constexpr int64_t kMostExpandedBytes = (int64_t)4 << 30;  // of the heads expanded at a time
 
 int build_prompt(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, int stride, const int32_t* group, const int32_t* prefix,
                  const int32_t* suffix, const int32_t* new_len, int64_t n_pool_pages, hipStream_t s, taper_latent_plan* plan) {
@@ -342,6 +342,10 @@ int build_prompt(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, 
             plan->e_page.push_back(b.block_table[(size_t)seq * stride + entry0 + j]);
             plan->e_valid.push_back(std::min(P, n_tokens - j * P));
         }
+        if (plan->e_page.size() % 2) {  // pages go in pairs: one without tokens
+            plan->e_page.push_back(plan->e_page.back());
+            plan->e_valid.push_back(0);
+        }
         return at;
     };
     int row0 = 0;
@@ -361,7 +365,7 @@ int build_prompt(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, 
                 t.prefix_e = prefix_e;
                 t.suffix_e = suffix_e;
                 t.page_begin = 0;
-                t.page_end = npre + (t.first_pos + t.n_rows - pl + P - 1) / P;
+                t.page_end = (npre + 1) / 2 * 2 + (t.first_pos + t.n_rows - pl + P - 1) / P;
                 t.part_row = -1;
                 t.n_pieces = 1;
                 plan->tiles.push_back(t);
@@ -382,7 +386,9 @@ int build_prompt(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, 
     lay.add(plan->tiles.data(), plan->tiles.size() * sizeof(taper::PromptTile));
     lay.add(plan->merges.data(), plan->merges.size() * sizeof(taper::PromptTile));
     const size_t image = lay.total();
+    const int64_t n_chunks = ((int64_t)plan->e_page.size() + 3) / 4;
     lay.add(nullptr, (size_t)head_bytes * plan->heads_at_once);
+    lay.add(nullptr, (size_t)n_chunks * plan->heads_at_once * 8);
     lay.add(nullptr, (size_t)plan->n_partial_rows * plan->heads_at_once * sizeof(float2));
     lay.add(nullptr, (size_t)plan->n_partial_rows * plan->heads_at_once * cfg.head_dim * sizeof(float));
     plan->device_bytes = (int64_t)lay.total();
@@ -397,8 +403,11 @@ int build_prompt(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, 
     a.tiles = (const taper::PromptTile*)lay.at(d, 2);
     a.merges = (const taper::PromptTile*)lay.at(d, 3);
     a.kv = lay.at(d, 4);
-    a.ml = (float2*)lay.at(d, 5);
-    a.part = (float*)lay.at(d, 6);
+    a.format = (int32_t*)lay.at(d, 5);
+    a.ml = (float2*)lay.at(d, 6);
+    a.part = (float*)lay.at(d, 7);
+    a.n_chunks = (int32_t)n_chunks;
+    a.units = ctx->units;
     a.n_expanded = (int32_t)plan->e_page.size();
     a.n_tiles = (int32_t)plan->tiles.size();
     a.n_merges = (int32_t)plan->merges.size();

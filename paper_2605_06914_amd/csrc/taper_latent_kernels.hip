@@ -82,12 +82,6 @@ __global__ __launch_bounds__(64) void absorb_kernel(const LatentShape sh, const 
 // ds_read_b64_tr_b16 reads 4 tokens x 16 columns transposed.
 // ---------------------------------------------------------------------------
 constexpr int kDecodeWaves = 8;
-// A partial row travels divided by its own sum, in half precision after division by a power of two of each wave's R / 8 columns that
-// brings their largest magnitude into [0.5, 1): off by 2^-12 of that, whatever the magnitude, and half the bytes of fp32 rows.
-DEV int exponent_of(float most) {
-    const int e = (int)((__float_as_uint(most) >> 23) & 0xff) - 126;
-    return e < -126 ? -126 : (e > 126 ? 126 : e);
-}
 template <int R>
 struct DecodeSmem {
     // (the small ones first: an LDS access has 16 bits of offset, and addresses beyond it cost a register each)
@@ -285,6 +279,8 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
             for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(O[k][d][i]));
         }
         const int e = exponent_of(max_lane_groups(most));
+        // the row travels divided by its own sum, in half precision after division by a power of two of each eighth of its columns that
+        // brings their largest magnitude into [0.5, 1): off by 2^-12 of that, whatever the magnitude, and half the bytes of fp32 rows
         PartStats* const st = a.stats + at;
         if (g == 0) st->exponent[wave] = (signed char)e;
         if (wave == 0 && g == 0) {

@@ -1,146 +1,236 @@
 // gfx950 kernels of a prompt's attention over a latent cache, in expanded form.
 //
 // expand_kernel makes every head's keys without rotation and values of every cached token that a new token sees (a shared prefix
-// once for all branches of its request), some heads at a time, in the tile layouts that the attention's matrix operands have: K
-// [d / 8][16 tokens][8], V [16 / 4][d][4].  prompt_kernel is causal attention of tiles of 128 query rows over them; the rotated
-// key parts come from the cache itself.  Where there are too few tiles for the chip their keys are cut into pieces, which
-// prompt_merge_kernel brings together.
+// once for all branches of its request), some heads at a time, in the layouts that the attention's matrix operands have: pages in
+// pairs, [K of the first: [d / 8][16 tokens][8]][K of the second][V: [4 lane groups][d][4 tokens of the first, 4 of the second]].
+// prompt_kernel is causal attention of tiles of query rows over them; the rotated key parts come from the cache itself.  Where there
+// are too few tiles for the chip their keys are cut into pieces, which prompt_merge_kernel brings together.
+//
+// Expanded keys and values are half precision, and so are the weights they meet: 11 bits of each instead of bf16's 8.  Four pages
+// whose keys (or values) half precision does not hold, beyond 65504 or all of them below 2^-10, are bf16 instead; `format` says
+// which.  A query's part without rotation is brought into half precision's range by a power of two of its own, exactly.
 #include <cmath>
+#include <type_traits>
 
 #include "latent_device.h"
 
 namespace taper {
 namespace latent {
 
-// ---------------------------------------------------------------------------
-// expand: a product of (tokens x R) and (R x 2 head_dim) for each head.  A workgroup takes 8 pages x 128 rows of W, 64 values of the
-// contraction at a time, both sides through LDS; a wave 4 pages x 64 rows.  Keys come out as W C^T (a lane: 4 consecutive d of a
-// token), values as C W^T (4 consecutive tokens of a d): both are 8 bytes of their tile.  A page's 64 values are 2 KiB in a row and
-// in operand order as they are; W's rows are 128 bytes each, their 16-byte pieces swapped about by the row so that 16 rows' pieces
-// lie in different banks.
-// ---------------------------------------------------------------------------
-struct ExpandSmem {
-    __bf16 c[2][8][8 * 128];  // [page][8 groups of 8 values][16 tokens][8]
-    __bf16 w[2][128][64];
-};
+typedef std::true_type yes;
+typedef std::false_type no;
+DEV f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+DEV float max_wave(float v) {
+#pragma unroll
+    for (int x = 32; x; x >>= 1) v = fmaxf(v, __shfl_xor(v, x));
+    return v;
+}
 
-template <int HD>
-__global__ __launch_bounds__(256, 2) void expand_kernel(const LatentShape sh, const PromptArgs a, const int h0, const int n_heads) {
-    __shared__ ExpandSmem sm;
-    const int R = sh.latent_dim, KD = R + kRopeDim;
-    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-    const int e0 = blockIdx.x / n_heads * 8, hl = blockIdx.x % n_heads, part = blockIdx.y;
-    const char* w = (const char*)((const __bf16*)a.w_up + ((int64_t)(h0 + hl) * 2 * HD + part * 128) * R);
-    int64_t page[2];
+// ---------------------------------------------------------------------------
+// expand: a product of (tokens x R) and (R x 2 head_dim) for each head.  A workgroup keeps 128 rows of W in LDS (R = 512: 128 KiB,
+// read 1 KiB an operand, each 16-byte piece moved by its row so that 8 rows' pieces lie in different banks) and its 8 waves go through
+// the tokens 64 at a time, each by itself: a page's operands come straight from the cache, 1 KiB in a row each, and nothing but W is
+// shared, so no wave waits for another.  Keys come out as W C^T (a lane: 4 consecutive d of a token), values as C W^T (4 consecutive
+// tokens of a d).
+// ---------------------------------------------------------------------------
+template <int R, int HD, int KIND>  // KIND 0: keys, 1: values, 2: 64 rows of keys, then 64 of values
+DEV void expand_chunk(const PromptArgs& a, const __bf16* w, const int hl, const int chunk) {
+    constexpr int KD = R + kRopeDim, KSTEPS = R / 32, AHEAD = 2;
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    auto is_value = [](int j) { return KIND == 1 || (KIND == 2 && j >= 4); };
+    const __bf16* page[4];
+    int valid[4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) page[i] = (int64_t)uniform(a.e_page[min(e0 + 2 * wave + i, a.n_expanded - 1)]) * KD * 32;
-    const int wrow = lane >> 3, wpiece = (lane & 7) ^ (wrow & 7);
-    auto fetch = [&](int k, int b) {  // values 64 k .. of both sides
+    for (int i = 0; i < 4; ++i) {
+        const int e = min(4 * chunk + i, a.n_expanded - 1);
+        page[i] = (const __bf16*)a.pages + (int64_t)uniform(a.e_page[e]) * (KD * 16) + g * 128 + n * 8;
+        valid[i] = a.e_valid[e];
+    }
+    const __bf16* w_at[2][2];  // where this lane reads W for even and odd steps, its first and its last 64 rows
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            load_to_lds((const char*)a.pages + page[i >> 1] + k * 2048, (i & 1) * 1024 + lane * 16, uniform(lds_address(&sm.c[b][2 * wave + (i >> 1)][0])) + (i & 1) * 1024);
+    for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            load_to_lds(w + k * 128, ((32 * wave + 8 * i + wrow) * R + wpiece * 8) * 2, uniform(lds_address(&sm.w[b][32 * wave + 8 * i][0])));
-    };
-    const int p0 = (wave & 1) * 4, r0 = (wave >> 1) * 64;
-    const bool values = part * 128 + r0 >= HD;
-    f32x4 acc[4][4];
+        for (int y = 0; y < 2; ++y) w_at[x][y] = w + (64 * y + n) * R + ((4 * x + g) ^ (n & 7)) * 8;
+    f32x4 acc[4][8];
+    bf16x8 cf[AHEAD][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) cf[k][i] = *(const bf16x8*)(page[i] + k * 512);
+    }
+#pragma unroll
+    for (int k = 0; k < KSTEPS; ++k) {
+        bf16x8 c[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            c[i] = cf[k % AHEAD][i];
+            if (k + AHEAD < KSTEPS) cf[k % AHEAD][i] = *(const bf16x8*)(page[i] + (k + AHEAD) * 512);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bf16x8 wf = *(const bf16x8*)(w_at[k & 1][j / 4] + (16 * (j % 4)) * R + (k >> 1) * 64);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i][j] = is_value(j) ? mfma16(c[i], wf, acc[i][j]) : mfma16(wf, c[i], acc[i][j]);
+        }
+        __builtin_amdgcn_sched_barrier(0);  // (else more of W is read ahead than there are registers for)
+    }
+    float most[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    fetch(0, 0);
-    for (int k = 0; k < R / 64; ++k) {
-        wait_loads_and_meet<0>();
-        if (k + 1 < R / 64) fetch(k + 1, (k + 1) & 1);
-        const int b = k & 1;
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            bf16x8 cf[4], wf[4];
+            for (int x = 0; x < 4; ++x) {
+                const float v = (is_value(j) ? 4 * g + x : n) < valid[i] ? acc[i][j][x] : 0.f;  // (slots past a length may hold anything)
+                acc[i][j][x] = v;
+                most[is_value(j)] = fmaxf(most[is_value(j)], fabsf(v));
+            }
+    bool wide[2] = {false, false};  // not for half precision
 #pragma unroll
-            for (int i = 0; i < 4; ++i) cf[i] = *(const bf16x8*)&sm.c[b][p0 + i][(4 * kk + g) * 128 + n * 8];
+    for (int v = 0; v < 2; ++v) {
+        if (KIND != 2 && KIND != v) continue;
+        const float m = max_wave(most[v]);
+        wide[v] = uniform(m > 65504.f || (m > 0.f && m < 0x1p-10f));
+        if (lane == 0) a.format[((int64_t)hl * a.n_chunks + chunk) * 2 + v] = wide[v];
+    }
+    auto store = [&](auto kind, auto convert) {  // (the operands' types: every value is rounded once)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) wf[j] = *(const bf16x8*)&sm.w[b][r0 + 16 * j + n][((4 * kk + g) ^ (n & 7)) * 8];
-            if (values) {
+        for (int pair = 0; pair < 2; ++pair) {
+            if (4 * chunk + 2 * pair >= a.n_expanded) return;
+            uint16_t* to = (uint16_t*)a.kv + ((int64_t)hl * (a.n_expanded / 2) + 2 * chunk + pair) * (64 * HD);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+            for (int j = 0; j < 8; ++j) {
+                if (is_value(j) != decltype(kind)::value) continue;
+                const int d = 16 * j - (KIND == 2 && is_value(j) ? 64 : 0);
+                if constexpr (decltype(kind)::value) {
+                    const uint2 x = convert(acc[2 * pair][j]), y = convert(acc[2 * pair + 1][j]);
+                    *(uint4*)(to + 32 * HD + (g * HD + d + n) * 8) = make_uint4(x.x, x.y, y.x, y.y);
+                } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[i][j] = mfma16(cf[i], wf[j], acc[i][j]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[i][j] = mfma16(wf[j], cf[i], acc[i][j]);
+                    for (int i = 0; i < 2; ++i) *(uint2*)(to + i * 16 * HD + ((d + 4 * g) >> 3) * 128 + n * 8 + (g & 1) * 4) = convert(acc[2 * pair + i][j]);
+                }
             }
         }
+    };
+    auto half = [](f32x4 v) { return __builtin_bit_cast(uint2, __builtin_convertvector(v, f16x4)); };
+    auto brain = [](f32x4 v) { return __builtin_bit_cast(uint2, __builtin_convertvector(v, bf16x4)); };
+    if (KIND != 1) {
+        if (wide[0]) store(no(), brain);
+        else store(no(), half);
     }
-    const int d0 = (part * 128 + r0) % HD;
+    if (KIND != 0) {
+        if (wide[1]) store(yes(), brain);
+        else store(yes(), half);
+    }
+}
+
+template <int R, int HD>
+__global__ __launch_bounds__(512, 2) void expand_kernel(const PromptArgs a, const int h0, const int n_heads) {
+    __shared__ __align__(16) __bf16 w[128 * R];
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int hl = blockIdx.x % n_heads, split = blockIdx.x / n_heads, part = blockIdx.y;
+    const char* from = (const char*)((const __bf16*)a.w_up + ((int64_t)(h0 + hl) * 2 * HD + part * 128) * R);
+    constexpr int ROWS = 512 / R;  // rows of W in a KiB
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int e = e0 + p0 + i;
-        if (e >= a.n_expanded) continue;
-        const int valid = a.e_valid[e];
-        __bf16* to = (__bf16*)a.kv + ((int64_t)hl * a.n_expanded + e) * (32 * HD);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            f32x4 v = acc[i][j];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) v[x] = (values ? 4 * g + x : n) < valid ? v[x] : 0.f;  // (slots past a length may hold anything)
-            const bf16x4 o = __builtin_convertvector(v, bf16x4);  // (the matrix operand's type)
-            const int d = d0 + 16 * j;
-            if (values) *(bf16x4*)(to + 16 * HD + g * 4 * HD + (d + n) * 4) = o;
-            else *(bf16x4*)(to + ((d + 4 * g) >> 3) * 128 + n * 8 + (g & 1) * 4) = o;
+    for (int i = 0; i < 16 / ROWS; ++i) {
+        const int row = (i * 8 + wave) * ROWS, mine = row + lane * ROWS / 64;
+        load_to_lds(from + row * R * 2, (mine - row) * R * 2 + ((lane % (64 / ROWS)) ^ (mine & 7)) * 16, uniform(lds_address(w + row * R)));
+    }
+    wait_loads_and_meet<0>();
+    const int n_waves = gridDim.x / n_heads * 8;
+    for (int c = split * 8 + wave; c < a.n_chunks; c += n_waves) {
+        if constexpr (HD == 64) {
+            expand_chunk<R, HD, 2>(a, w, hl, c);
+        } else if (part == 0) {
+            expand_chunk<R, HD, 0>(a, w, hl, c);
+        } else {
+            expand_chunk<R, HD, 1>(a, w, hl, c);
         }
     }
 }
 
 // ---------------------------------------------------------------------------
-// The attention: 4 waves of 32 query rows, 64 tokens (4 pages) at a time through LDS, everything transposed as in the decode kernels:
-// S^T = K Q^T leaves the weights in the layout that O^T = V^T P^T takes them in.
+// The attention: 8 waves of 32 query rows, 64 tokens (4 pages) at a time through LDS, two such tiles on their way behind the one at
+// hand (with one, half of the time went by in waits), everything transposed as in the decode kernels: S^T = K Q^T leaves the weights in
+// the layout that O^T = V^T P^T takes them in.
 // ---------------------------------------------------------------------------
+constexpr int kStages = 3;
 template <int HD>
 struct PromptSmem {
-    __bf16 k[2][4][HD * 16];
-    __bf16 r[2][4][kRopeDim * 16];
-    __bf16 v[2][4][HD * 16];
+    _Float16 k[kStages][4][HD * 16];
+    __bf16 r[kStages][4][kRopeDim * 16];
+    _Float16 v[kStages][2][HD * 32];
 };
 
 template <int HD>
-__global__ __launch_bounds__(256, 2) void prompt_kernel(const LatentShape sh, const PromptArgs a, const int h0, const int n_heads) {
-    constexpr int KS = HD / 32, DT = HD / 16, NT = 2;
+__global__ __launch_bounds__(512, 2) void prompt_kernel(const LatentShape sh, const PromptArgs a, const int h0, const int n_heads) {
+    constexpr int KS = HD / 32, DT = HD / 16, NT = 2, LOADS = HD / 32 + 1;  // LOADS: KiB of half a page
     __shared__ PromptSmem<HD> sm;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     const int hl = blockIdx.x % n_heads, h = h0 + hl, H = sh.n_heads;
     const PromptTile t = a.tiles[blockIdx.x / n_heads];
-    const int npre = (t.prefix_len + 15) / 16;
-    const float c = sh.scale_log2e;
-    auto expanded = [&](int vp) { return vp < npre ? t.prefix_e + vp : t.suffix_e + (vp - npre); };
+    const int npre = (t.prefix_len + 31) / 32 * 2;  // (pages of the prefix, in pairs)
     const int64_t page_bytes = (sh.latent_dim + kRopeDim) * 32LL;
+    const scalar_row e_page = (scalar_row)a.e_page;
+    auto expanded = [&](int vp) { return vp < npre ? t.prefix_e + vp : t.suffix_e + (vp - npre); };
+    // a wave brings half of a page: keys and half of its rotated part, or the other half and a half of a pair's values
     auto fetch = [&](int vp0, int b) {
-        const int e = uniform(expanded(min(vp0 + wave, t.page_end - 1)));
-        const char* kv = (const char*)a.kv + ((int64_t)hl * a.n_expanded + e) * (64 * HD);
-        const char* rope = (const char*)a.pages + (int64_t)uniform(a.e_page[e]) * page_bytes + sh.latent_dim * 32;
-        const unsigned kl = uniform(lds_address(sm.k[b][wave])), vl = uniform(lds_address(sm.v[b][wave])), rl = uniform(lds_address(sm.r[b][wave]));
+        const int pg = wave >> 1, e = expanded(min(vp0 + pg, t.page_end - 1));
+        const char* kv = (const char*)a.kv + ((int64_t)hl * (a.n_expanded / 2) + e / 2) * (128 * HD);
+        const char* rope = (const char*)a.pages + (int64_t)e_page[e] * page_bytes + sh.latent_dim * 32;
+        if ((wave & 1) == 0) {
+            const unsigned to = uniform(lds_address(sm.k[b][pg]));
 #pragma unroll
-        for (int i = 0; i < HD / 32; ++i) load_to_lds(kv, i * 1024 + lane * 16, kl + i * 1024);
+            for (int i = 0; i < HD / 32; ++i) load_to_lds(kv + (e & 1) * (32 * HD) + i * 1024, lane * 16, to + i * 1024);
+            load_to_lds(rope, lane * 16, uniform(lds_address(sm.r[b][pg])));
+        } else {
+            const unsigned to = uniform(lds_address(sm.v[b][pg >> 1])) + (pg & 1) * (32 * HD);
+            load_to_lds(rope + 1024, lane * 16, uniform(lds_address(sm.r[b][pg])) + 1024);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) load_to_lds(rope, i * 1024 + lane * 16, rl + i * 1024);
-#pragma unroll
-        for (int i = 0; i < HD / 32; ++i) load_to_lds(kv + 32 * HD, i * 1024 + lane * 16, vl + i * 1024);
+            for (int i = 0; i < HD / 32; ++i) load_to_lds(kv + 64 * HD + (pg & 1) * (32 * HD) + i * 1024, lane * 16, to + i * 1024);
+        }
     };
+    const int n_tiles = (t.page_end - t.page_begin + 3) / 4;
     fetch(t.page_begin, 0);
-    bf16x8 qf[NT][KS + 2];
-    int pos[NT];  // of this lane's rows
+    if (n_tiles > 1) fetch(t.page_begin + 4, 1);
+    f16x8 qf[NT][KS];
+    bf16x8 qr[NT][2];
+    int pos[NT];   // of this lane's rows
+    float c[NT];   // scale * log2(e) * the power of two its query was divided by
 #pragma unroll
     for (int k = 0; k < NT; ++k) {
         const int r = min(32 * wave + 16 * k + n, t.n_rows - 1);
         pos[k] = t.first_pos + r;
         const __bf16* q = (const __bf16*)a.q + ((int64_t)(t.row0 + r) * H + h) * (HD + kRopeDim) + 8 * g;
+        typedef float f32x8 __attribute__((ext_vector_type(8)));
+        f32x8 v[KS];
+        float most = 0.f;
 #pragma unroll
-        for (int j = 0; j < KS + 2; ++j) qf[k][j] = *(const bf16x8*)(q + 32 * j);
+        for (int j = 0; j < KS; ++j) {
+            v[j] = __builtin_convertvector(*(const bf16x8*)(q + 32 * j), f32x8);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(v[j][i]));
+        }
+        const int e = exponent_of(max_lane_groups(most));
+        const float down = __uint_as_float((unsigned)(127 - e) << 23);
+        c[k] = sh.scale_log2e * __uint_as_float((unsigned)(127 + e) << 23);
+#pragma unroll
+        for (int j = 0; j < KS; ++j) qf[k][j] = __builtin_convertvector(v[j] * down, f16x8);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            qr[k][j] = __builtin_convertvector(__builtin_convertvector(*(const bf16x8*)(q + HD + 32 * j), f32x8) * down, bf16x8);
     }
-    const int first_pos = t.first_pos + min(32 * wave, t.n_rows - 1);  // of this wave's rows
+    const int first_pos = t.first_pos + min(32 * wave, t.n_rows - 1), last_pos = t.first_pos + min(32 * wave + 31, t.n_rows - 1);  // of this wave's rows
+    const bool idle = 32 * wave >= t.n_rows;
+    int some = 0;  // pages in bf16 among those of this tile?
+    {
+        const int* format = a.format + (int64_t)hl * a.n_chunks * 2;
+        const int p_end = (t.prefix_e + min(t.page_end, npre) + 3) / 4, s_end = (t.suffix_e + max(t.page_end - npre, 0) + 3) / 4;
+        for (int i = t.prefix_e / 4 * 2 + lane; i < 2 * p_end; i += 64) some |= format[i];
+        for (int i = t.suffix_e / 4 * 2 + lane; i < 2 * s_end; i += 64) some |= format[i];
+    }
     f32x4 O[NT][DT];
     float m[NT], l[NT];
 #pragma unroll
@@ -150,20 +240,46 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const LatentShape sh, co
 #pragma unroll
         for (int d = 0; d < DT; ++d) O[k][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    for (int vp0 = t.page_begin, b = 0; vp0 < t.page_end; vp0 += 4, b ^= 1) {
-        wait_loads_and_meet<0>();  // this tile is here for all, and all are done with the one before
-        if (vp0 + 4 < t.page_end) fetch(vp0 + 4, b ^ 1);
+    auto tile = [&](const int vp0, const int b, auto plain) {
+        constexpr bool PLAIN = decltype(plain)::value;
+        int format[4] = {0, 0, 0, 0};  // per pair: keys, values
+        if constexpr (!PLAIN)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                format[i] = ((scalar_row)a.format)[((int64_t)hl * a.n_chunks + expanded(min(vp0 + (i & 2), t.page_end - 1)) / 4) * 2 + (i & 1)];
         f32x4 s[4][NT];
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
 #pragma unroll
             for (int k = 0; k < NT; ++k) s[p][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (PLAIN || !format[p & 2]) {
 #pragma unroll
-            for (int j = 0; j < KS + 2; ++j) {
-                const __bf16* from = j < KS ? sm.k[b][p] + (4 * j + g) * 128 : sm.r[b][p] + (4 * (j - KS) + g) * 128;
-                const bf16x8 kf = *(const bf16x8*)(from + n * 8);
+                for (int j = 0; j < KS; ++j) {
+                    const f16x8 kf = *(const f16x8*)(sm.k[b][p] + (4 * j + g) * 128 + n * 8);
 #pragma unroll
-                for (int k = 0; k < NT; ++k) s[p][k] = mfma16(kf, qf[k][j], s[p][k]);
+                    for (int k = 0; k < NT; ++k) s[p][k] = mfma16(kf, qf[k][j], s[p][k]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < KS; ++j) {
+                    const bf16x8 kf = *(const bf16x8*)(sm.k[b][p] + (4 * j + g) * 128 + n * 8);
+#pragma unroll
+                    for (int k = 0; k < NT; ++k) {
+                        u32x4 bits = __builtin_bit_cast(u32x4, qf[k][j]);
+                        asm volatile("" : "+v"(bits));  // (converted here each time: there are no registers to keep the results)
+                        const f16x8 h = __builtin_bit_cast(f16x8, bits);
+                        bf16x8 q;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) q[i] = (__bf16)(float)h[i];  // (they were bf16)
+                        s[p][k] = mfma16(kf, q, s[p][k]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const bf16x8 kf = *(const bf16x8*)(sm.r[b][p] + (4 * j + g) * 128 + n * 8);
+#pragma unroll
+                for (int k = 0; k < NT; ++k) s[p][k] = mfma16(kf, qr[k][j], s[p][k]);
             }
         }
         // pages that hold tokens ahead of some row, none at all, or the end of a prefix
@@ -172,23 +288,21 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const LatentShape sh, co
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
                 const int vp = vp0 + p;
-                // positions of the page begin at `from`; those of a prefix end with it, and a page that is not there has none
-                const int from = vp < npre ? 16 * vp : t.prefix_len + 16 * (vp - npre);
+                // positions of the page begin at `first`; those of a prefix end with it, and a page that is not there has none
+                const int first = vp < npre ? 16 * vp : t.prefix_len + 16 * (vp - npre);
                 const int most = vp >= t.page_end ? -1 : vp < npre ? t.prefix_len - 1 : 0x7fffffff;
 #pragma unroll
                 for (int k = 0; k < NT; ++k)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) s[p][k][i] = from + 4 * g + i <= min(pos[k], most) ? s[p][k][i] : -INFINITY;
+                    for (int i = 0; i < 4; ++i) s[p][k][i] = first + 4 * g + i <= min(pos[k], most) ? s[p][k][i] : -INFINITY;
             }
         }
-        bf16x4 pr[4][NT];
+        uint2 pr[4][NT];
 #pragma unroll
         for (int k = 0; k < NT; ++k) {
-            float mx = -INFINITY;
-#pragma unroll
-            for (int p = 0; p < 4; ++p) mx = fmaxf(fmaxf(mx, fmaxf(s[p][k][0], s[p][k][1])), fmaxf(s[p][k][2], s[p][k][3]));
-            if (__any(mx * c > m[k])) {
-                const float mn = fmaxf(m[k], max_lane_groups(mx) * c);
+            const float mx = max2(max2(max4(s[0][k]), max4(s[1][k])), max2(max4(s[2][k]), max4(s[3][k])));
+            if (__any(!(mx * c[k] <= m[k]))) {
+                const float mn = max2(m[k], max_lane_groups(mx) * c[k]);
                 const float alpha = fast_exp2(m[k] - (mn == -INFINITY ? 0.f : mn));
                 l[k] *= alpha;
 #pragma unroll
@@ -200,21 +314,38 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const LatentShape sh, co
             for (int p = 0; p < 4; ++p) {
                 f32x4 w;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = fast_exp2(fmaf(s[p][k][i], c, -ref));
+                for (int i = 0; i < 4; ++i) w[i] = fast_exp2(fmaf(s[p][k][i], c[k], -ref));
                 l[k] += (w[0] + w[1]) + (w[2] + w[3]);
-                pr[p][k] = __builtin_convertvector(w, bf16x4);  // (weights of at most 1, in 8 bits each)
+                // (weights of at most 1, in the type of the values they meet)
+                pr[p][k] = PLAIN || !format[(p & 2) + 1] ? __builtin_bit_cast(uint2, __builtin_convertvector(w, f16x4)) : __builtin_bit_cast(uint2, __builtin_convertvector(w, bf16x4));
             }
         }
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
-                const int at = g * 4 * HD + (16 * d + n) * 4;
-                const bf16x8 vf = cat(*(const bf16x4*)(sm.v[b][2 * ks] + at), *(const bf16x4*)(sm.v[b][2 * ks + 1] + at));
+                const uint4 vf = *(const uint4*)(sm.v[b][ks] + (g * HD + 16 * d + n) * 8);
 #pragma unroll
-                for (int k = 0; k < NT; ++k) O[k][d] = mfma16(vf, cat(pr[2 * ks][k], pr[2 * ks + 1][k]), O[k][d]);
+                for (int k = 0; k < NT; ++k) {
+                    const uint4 pf = make_uint4(pr[2 * ks][k].x, pr[2 * ks][k].y, pr[2 * ks + 1][k].x, pr[2 * ks + 1][k].y);
+                    if (PLAIN || !format[2 * ks + 1]) O[k][d] = mfma16(__builtin_bit_cast(f16x8, vf), __builtin_bit_cast(f16x8, pf), O[k][d]);
+                    else O[k][d] = mfma16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pf), O[k][d]);
+                }
             }
-    }
+    };
+    auto all_tiles = [&](auto plain) {
+        for (int i = 0, b = 0; i < n_tiles; ++i, b = b == kStages - 1 ? 0 : b + 1) {
+            // this tile is here for all (the next may be on its way), and all are done with the one before, where the one after the next goes
+            if (i + 1 < n_tiles) wait_loads_and_meet<LOADS>();
+            else wait_loads_and_meet<0>();
+            const int vp0 = t.page_begin + 4 * i;
+            if (i + 2 < n_tiles) fetch(vp0 + 8, b == 0 ? kStages - 1 : b - 1);
+            const bool ahead = vp0 >= npre && t.prefix_len + 16 * (vp0 - npre) > last_pos;  // of all of this wave's rows
+            if (!ahead && !idle) tile(vp0, b, plain);
+        }
+    };
+    if (__any(some)) all_tiles(no());
+    else all_tiles(yes());
 #pragma unroll
     for (int k = 0; k < NT; ++k) {
         const int r = 32 * wave + 16 * k + n;
@@ -263,12 +394,15 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const LatentShape sh,
     }
 }
 
-template <int HD>
+template <int R, int HD>
 static hipError_t launch_prompt_as(const LatentShape& sh, const PromptArgs& a, hipStream_t s) {
     for (int h0 = 0; h0 < sh.n_heads; h0 += a.heads_at_once) {
         const int nh = sh.n_heads - h0 < a.heads_at_once ? sh.n_heads - h0 : a.heads_at_once;
-        hipLaunchKernelGGL(expand_kernel<HD>, dim3((unsigned)((a.n_expanded + 7) / 8) * nh, HD / 64), dim3(256), 0, s, sh, a, h0, nh);
-        hipLaunchKernelGGL(prompt_kernel<HD>, dim3((unsigned)a.n_tiles * nh), dim3(256), 0, s, sh, a, h0, nh);
+        // a workgroup a compute unit (two at R = 256), unless there are fewer tokens than that
+        const int parts = nh * (HD / 64), most = (a.n_chunks + 7) / 8, wish = a.units * (512 / R) / parts;
+        const int split = wish < 1 ? 1 : (wish > most ? most : wish);
+        hipLaunchKernelGGL((expand_kernel<R, HD>), dim3((unsigned)nh * split, HD / 64), dim3(512), 0, s, a, h0, nh);
+        hipLaunchKernelGGL(prompt_kernel<HD>, dim3((unsigned)a.n_tiles * nh), dim3(512), 0, s, sh, a, h0, nh);
         if (a.n_merges > 0) hipLaunchKernelGGL(prompt_merge_kernel<HD>, dim3((unsigned)a.n_merges * nh, 8), dim3(256), 0, s, sh, a, h0, nh);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -279,7 +413,9 @@ static hipError_t launch_prompt_as(const LatentShape& sh, const PromptArgs& a, h
 }  // namespace latent
 
 hipError_t launch_latent_prompt(const LatentShape& sh, const PromptArgs& a, hipStream_t s) {
-    return sh.head_dim == 128 ? latent::launch_prompt_as<128>(sh, a, s) : latent::launch_prompt_as<64>(sh, a, s);
+    using namespace latent;
+    if (sh.latent_dim == 512) return sh.head_dim == 128 ? launch_prompt_as<512, 128>(sh, a, s) : launch_prompt_as<512, 64>(sh, a, s);
+    return sh.head_dim == 128 ? launch_prompt_as<256, 128>(sh, a, s) : launch_prompt_as<256, 64>(sh, a, s);
 }
 
 }  // namespace taper
