@@ -67,6 +67,13 @@ DEV void wait_loads_and_meet() {
 // LDS accesses are done and every wave is here; loads stay in flight.
 DEV void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// A per-lane value the compiler must not reason about: what is derived from it is computed where it is used, and not kept in registers
+// from earlier on.
+DEV int opaque(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // Integers of a plan, which no kernel writes: read by scalar loads.
 typedef const __attribute__((address_space(4))) int32_t* scalar_row;
 

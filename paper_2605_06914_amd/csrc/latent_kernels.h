@@ -39,6 +39,10 @@ struct LatentDecodeArgs {
 };
 hipError_t launch_latent_decode(const LatentShape& sh, const LatentDecodeArgs& a, hipStream_t s);
 
+// The normaliser of a row that sees few tokens feels the rounding of their keys, which averages out over many (at 128 tokens and unit
+// scores it is off by 2e-5 of some 5): pages that hold positions below this have low parts of their keys, which such rows add.
+constexpr int kLowPositions = 128;
+
 // A tile of a prompt's query rows.
 struct PromptTile {
     int32_t row0, n_rows;        // rows of q
@@ -48,13 +52,16 @@ struct PromptTile {
     int32_t page_begin, page_end;  // the pages (of the prefix, an even number, then private ones) this tile's item meets; page_begin is even
     int32_t part_row;            // partial rows of head 0, or -1: the item is its rows' only one and writes the result
     int32_t n_pieces;            // items of the same rows; their partial rows are n_rows apart
+    int32_t bundle, n_bundle;    // this item is one of n_bundle from number `bundle` on that meet the same keys (see tile_of_block)
 };
 struct PromptArgs {
     const int32_t* e_page;       // [n_expanded] physical page of an expanded page
     const int32_t* e_valid;      // [n_expanded] tokens of it that exist
+    const int32_t* e_low;        // [n_expanded] number of its page of low parts, -1: it has none
     const PromptTile* tiles;     // [n_tiles], longest first
     const PromptTile* merges;    // [n_merges] row tiles whose keys are cut into pieces
     void* kv;                    // [head of the group][n_expanded / 2][K, K, V of a pair of pages] (see the kernels)
+    void* k_low;                 // f16 [head of the group][n_low][K]: 2^11 times what the rounding of keys took away, where lse is wanted
     int32_t* format;             // [head of the group][n_chunks][keys, values]: 1 where four pages are bf16 instead of half precision
     float2* ml;
     float* part;                 // [head][partial rows][head_dim]
@@ -64,6 +71,7 @@ struct PromptArgs {
     void* out;
     float* lse;
     int32_t n_chunks, units;     // fours of expanded pages; compute units
+    int32_t n_low;               // pages of low parts
     int32_t n_expanded, n_tiles, n_merges, n_partial_rows;  // partial rows of one head
     int32_t heads_at_once;
 };

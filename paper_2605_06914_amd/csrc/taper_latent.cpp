@@ -60,7 +60,8 @@ struct taper_latent_plan {
     int64_t n_partial_rows = 0;
     // prompt
     std::vector<taper::PromptTile> tiles, merges;
-    std::vector<int32_t> e_page, e_valid;
+    std::vector<int32_t> e_page, e_valid, e_low;
+    int32_t n_low = 0;
     int64_t n_rows = 0;
     int heads_at_once = 0;
     // device
@@ -318,6 +319,60 @@ int build_decode(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, 
 constexpr int kPromptRows = 256;
 constexpr int64_t kMostExpandedBytes = (int64_t)4 << 30;  // of the heads expanded at a time
 
+constexpr int kLeastPiecePages = 16;  // a piece's start and its partial rows cost about as much as so many pages
+constexpr int kMostBundle = 8;        // items side by side: what an XCD's 32 compute units hold of four heads
+constexpr double kBundleLeast = 0.75;  // the shortest of them, relative to the longest (shorter ones are better kept for the end)
+
+// From the row tiles (in the order of their sequences' rows) to items: tiles with more than a unit's equal share of the keys are cut into
+// pieces; items that meet the same keys at the same time are bundled; the longest bundles come first.
+void make_prompt_items(int units, taper_latent_plan* plan) {
+    std::vector<taper::PromptTile> rows;
+    rows.swap(plan->tiles);
+    int64_t pages = 0;
+    for (const taper::PromptTile& t : rows) pages += t.page_end;
+    const int64_t share = std::max<int64_t>(kLeastPiecePages, (pages * plan->heads_at_once + units - 1) / units);
+    std::vector<std::vector<taper::PromptTile>> bundles;
+    size_t e = rows.size();
+    while (e > 0) {  // from the longest tile of a sequence down
+        const int longest = rows[e - 1].page_end, n_pieces = (int)((longest + share - 1) / share);
+        size_t i = e - 1;
+        while (i > 0 && e - i < (size_t)kMostBundle && rows[i - 1].suffix_e == rows[e - 1].suffix_e && rows[i - 1].page_end > kBundleLeast * longest) --i;
+        const int per = ((longest + n_pieces - 1) / n_pieces + 3) / 4 * 4;
+        for (size_t j = i; j < e; ++j) {
+            taper::PromptTile& t = rows[j];
+            t.n_pieces = (t.page_end + per - 1) / per;
+            if (t.n_pieces == 1) continue;
+            t.part_row = (int32_t)plan->n_partial_rows;
+            plan->n_partial_rows += (int64_t)t.n_pieces * t.n_rows;
+            plan->merges.push_back(t);
+        }
+        for (int k = 0; k < n_pieces; ++k) {
+            std::vector<taper::PromptTile> bundle;
+            for (size_t j = i; j < e; ++j) {
+                taper::PromptTile t = rows[j];
+                if (k >= t.n_pieces) continue;
+                if (t.n_pieces > 1) t.part_row += k * t.n_rows;
+                t.page_begin = k * per;
+                t.page_end = std::min(t.page_end, (k + 1) * per);
+                bundle.push_back(t);
+            }
+            if (!bundle.empty()) bundles.push_back(bundle);
+        }
+        e = i;
+    }
+    std::stable_sort(bundles.begin(), bundles.end(), [](const std::vector<taper::PromptTile>& x, const std::vector<taper::PromptTile>& y) {
+        return x.back().page_end - x.back().page_begin > y.back().page_end - y.back().page_begin;
+    });
+    for (const auto& bundle : bundles) {
+        const int32_t first = (int32_t)plan->tiles.size();
+        for (taper::PromptTile t : bundle) {
+            t.bundle = first;
+            t.n_bundle = (int32_t)bundle.size();
+            plan->tiles.push_back(t);
+        }
+    }
+}
+
 int build_prompt(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, int stride, const int32_t* group, const int32_t* prefix,
                  const int32_t* suffix, const int32_t* new_len, int64_t n_pool_pages, hipStream_t s, taper_latent_plan* plan) {
     const taper_latent_config& cfg = ctx->cfg;
@@ -336,15 +391,17 @@ int build_prompt(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, 
     }
     if (plan->n_rows == 0) return set_error(TAPER_ELEN, "no sequence has a new token");
     if (plan->n_rows > INT32_MAX / cfg.n_heads) return set_error(TAPER_ELEN, "too many query rows");
-    auto expand = [&](int seq, int entry0, int n_tokens) {
+    auto expand = [&](int seq, int entry0, int n_tokens, int position) {  // (of the first token)
         const int at = (int)plan->e_page.size();
         for (int j = 0; j * P < n_tokens; ++j) {
             plan->e_page.push_back(b.block_table[(size_t)seq * stride + entry0 + j]);
             plan->e_valid.push_back(std::min(P, n_tokens - j * P));
+            plan->e_low.push_back(position + j * P < taper::kLowPositions ? plan->n_low++ : -1);
         }
         if (plan->e_page.size() % 2) {  // pages go in pairs: one without tokens
             plan->e_page.push_back(plan->e_page.back());
             plan->e_valid.push_back(0);
+            plan->e_low.push_back(-1);
         }
         return at;
     };
@@ -354,8 +411,8 @@ int build_prompt(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, 
         for (int q = b.group_start[g]; q < b.group_start[g + 1]; ++q) {
             const int pl = prefix[q], n = new_len[q], npre = b.n_prefix_pages[q];
             if (n == 0) continue;
-            if (prefix_e < 0) prefix_e = expand(q, 0, pl);
-            const int suffix_e = expand(q, npre, suffix[q]);
+            if (prefix_e < 0) prefix_e = expand(q, 0, pl, 0);
+            const int suffix_e = expand(q, npre, suffix[q], pl);
             for (int r = 0; r < n; r += kPromptRows) {
                 taper::PromptTile t;
                 t.row0 = row0 + r;
@@ -373,22 +430,22 @@ int build_prompt(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, 
             row0 += n;
         }
     }
-    std::stable_sort(plan->tiles.begin(), plan->tiles.end(), [](const taper::PromptTile& x, const taper::PromptTile& y) {
-        return x.page_end - x.page_begin > y.page_end - y.page_begin;
-    });
     const int64_t head_bytes = (int64_t)plan->e_page.size() * P * 2 * cfg.head_dim * 2;
     plan->heads_at_once = (int)std::max<int64_t>(1, std::min<int64_t>(cfg.n_heads, kMostExpandedBytes / head_bytes));
     if (plan->heads_at_once > 8) plan->heads_at_once -= plan->heads_at_once % 8 && plan->heads_at_once < cfg.n_heads ? plan->heads_at_once % 8 : 0;
-    if ((int64_t)std::max(plan->tiles.size(), plan->e_page.size()) * plan->heads_at_once > (int64_t)kMostBlocks) return set_error(TAPER_ELEN, "too many query rows");
+    make_prompt_items(ctx->units, plan);
+    if ((int64_t)std::max(plan->tiles.size(), plan->e_page.size()) * plan->heads_at_once > (int64_t)kMostBlocks || plan->n_partial_rows * plan->heads_at_once > INT32_MAX) return set_error(TAPER_ELEN, "too many query rows");
     Layout lay;
     lay.add(plan->e_page.data(), plan->e_page.size() * 4);
     lay.add(plan->e_valid.data(), plan->e_valid.size() * 4);
+    lay.add(plan->e_low.data(), plan->e_low.size() * 4);
     lay.add(plan->tiles.data(), plan->tiles.size() * sizeof(taper::PromptTile));
     lay.add(plan->merges.data(), plan->merges.size() * sizeof(taper::PromptTile));
     const size_t image = lay.total();
     const int64_t n_chunks = ((int64_t)plan->e_page.size() + 3) / 4;
     lay.add(nullptr, (size_t)head_bytes * plan->heads_at_once);
     lay.add(nullptr, (size_t)n_chunks * plan->heads_at_once * 8);
+    lay.add(nullptr, (size_t)plan->n_low * plan->heads_at_once * P * cfg.head_dim * 2);
     lay.add(nullptr, (size_t)plan->n_partial_rows * plan->heads_at_once * sizeof(float2));
     lay.add(nullptr, (size_t)plan->n_partial_rows * plan->heads_at_once * cfg.head_dim * sizeof(float));
     plan->device_bytes = (int64_t)lay.total();
@@ -400,12 +457,15 @@ int build_prompt(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, 
     std::memset(&a, 0, sizeof a);
     a.e_page = (const int32_t*)lay.at(d, 0);
     a.e_valid = (const int32_t*)lay.at(d, 1);
-    a.tiles = (const taper::PromptTile*)lay.at(d, 2);
-    a.merges = (const taper::PromptTile*)lay.at(d, 3);
-    a.kv = lay.at(d, 4);
-    a.format = (int32_t*)lay.at(d, 5);
-    a.ml = (float2*)lay.at(d, 6);
-    a.part = (float*)lay.at(d, 7);
+    a.e_low = (const int32_t*)lay.at(d, 2);
+    a.tiles = (const taper::PromptTile*)lay.at(d, 3);
+    a.merges = (const taper::PromptTile*)lay.at(d, 4);
+    a.kv = lay.at(d, 5);
+    a.format = (int32_t*)lay.at(d, 6);
+    a.k_low = lay.at(d, 7);
+    a.ml = (float2*)lay.at(d, 8);
+    a.part = (float*)lay.at(d, 9);
+    a.n_low = plan->n_low;
     a.n_chunks = (int32_t)n_chunks;
     a.units = ctx->units;
     a.n_expanded = (int32_t)plan->e_page.size();

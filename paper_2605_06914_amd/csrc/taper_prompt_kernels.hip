@@ -36,15 +36,16 @@ DEV float max_wave(float v) {
 template <int R, int HD, int KIND>  // KIND 0: keys, 1: values, 2: 64 rows of keys, then 64 of values
 DEV void expand_chunk(const PromptArgs& a, const __bf16* w, const int hl, const int chunk) {
     constexpr int KD = R + kRopeDim, KSTEPS = R / 32, AHEAD = 2;
-    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    int lane = opaque(threadIdx.x) & 63, n = lane & 15, g = lane >> 4;
     auto is_value = [](int j) { return KIND == 1 || (KIND == 2 && j >= 4); };
     const __bf16* page[4];
+    const int at = g * 128 + n * 8;
     int valid[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int e = min(4 * chunk + i, a.n_expanded - 1);
-        page[i] = (const __bf16*)a.pages + (int64_t)uniform(a.e_page[e]) * (KD * 16) + g * 128 + n * 8;
-        valid[i] = a.e_valid[e];
+        page[i] = (const __bf16*)a.pages + (int64_t)uniform(a.e_page[e]) * (KD * 16);
+        valid[i] = uniform(a.e_valid[e]);
     }
     const __bf16* w_at[2][2];  // where this lane reads W for even and odd steps, its first and its last 64 rows
 #pragma unroll
@@ -58,7 +59,7 @@ DEV void expand_chunk(const PromptArgs& a, const __bf16* w, const int hl, const 
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) cf[k][i] = *(const bf16x8*)(page[i] + k * 512);
+        for (int k = 0; k < AHEAD; ++k) cf[k][i] = *(const bf16x8*)(page[i] + at + k * 512);
     }
 #pragma unroll
     for (int k = 0; k < KSTEPS; ++k) {
@@ -66,7 +67,7 @@ DEV void expand_chunk(const PromptArgs& a, const __bf16* w, const int hl, const 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             c[i] = cf[k % AHEAD][i];
-            if (k + AHEAD < KSTEPS) cf[k % AHEAD][i] = *(const bf16x8*)(page[i] + (k + AHEAD) * 512);
+            if (k + AHEAD < KSTEPS) cf[k % AHEAD][i] = *(const bf16x8*)(page[i] + at + (k + AHEAD) * 512);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -76,6 +77,7 @@ DEV void expand_chunk(const PromptArgs& a, const __bf16* w, const int hl, const 
         }
         __builtin_amdgcn_sched_barrier(0);  // (else more of W is read ahead than there are registers for)
     }
+    lane = opaque(threadIdx.x) & 63, n = lane & 15, g = lane >> 4;  // (again: no registers for them in between)
     float most[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -114,6 +116,22 @@ DEV void expand_chunk(const PromptArgs& a, const __bf16* w, const int hl, const 
             }
         }
     };
+    if (KIND != 1 && a.lse) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int low = 4 * chunk + i < a.n_expanded ? uniform(a.e_low[4 * chunk + i]) : -1;
+            if (low < 0) continue;
+            uint16_t* to = (uint16_t*)a.k_low + ((int64_t)hl * a.n_low + low) * (16 * HD) + n * 8 + (g & 1) * 4;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (is_value(j)) continue;
+                f32x4 rest;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) rest[x] = wide[0] ? 0.f : (acc[i][j][x] - (float)(_Float16)acc[i][j][x]) * 0x1p11f;
+                *(uint2*)(to + ((16 * j + 4 * g) >> 3) * 128) = __builtin_bit_cast(uint2, __builtin_convertvector(rest, f16x4));
+            }
+        }
+    }
     auto half = [](f32x4 v) { return __builtin_bit_cast(uint2, __builtin_convertvector(v, f16x4)); };
     auto brain = [](f32x4 v) { return __builtin_bit_cast(uint2, __builtin_convertvector(v, bf16x4)); };
     if (KIND != 1) {
@@ -164,13 +182,30 @@ struct PromptSmem {
     _Float16 v[kStages][2][HD * 32];
 };
 
+// Which item and head a workgroup has.  Items that meet the same keys lie together (a bundle); of each head of a bundle the items
+// become workgroups 8 apart, so that they run on one XCD (workgroup i runs on XCD i mod 8) at about the same time and share its L2.
+DEV void tile_of_block(const PromptArgs& a, const int block, const int n_heads, int* tile, int* head) {
+    const PromptTile& t = a.tiles[block / n_heads];
+    const int b = t.bundle, n = t.n_bundle, u = block - b * n_heads, eights = n_heads / 8 * 8;
+    if (u < eights * n) {
+        *tile = b + u % (8 * n) / 8;
+        *head = u / (8 * n) * 8 + u % 8;
+    } else {
+        const int v = u - eights * n, rest = n_heads - eights;
+        *tile = b + v / rest;
+        *head = eights + v % rest;
+    }
+}
+
 template <int HD>
 __global__ __launch_bounds__(512, 2) void prompt_kernel(const LatentShape sh, const PromptArgs a, const int h0, const int n_heads) {
     constexpr int KS = HD / 32, DT = HD / 16, NT = 2, LOADS = HD / 32 + 1;  // LOADS: KiB of half a page
     __shared__ PromptSmem<HD> sm;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-    const int hl = blockIdx.x % n_heads, h = h0 + hl, H = sh.n_heads;
-    const PromptTile t = a.tiles[blockIdx.x / n_heads];
+    int hl, item;
+    tile_of_block(a, blockIdx.x, n_heads, &item, &hl);
+    const int h = h0 + hl, H = sh.n_heads;
+    const PromptTile t = a.tiles[item];
     const int npre = (t.prefix_len + 31) / 32 * 2;  // (pages of the prefix, in pairs)
     const int64_t page_bytes = (sh.latent_dim + kRopeDim) * 32LL;
     const scalar_row e_page = (scalar_row)a.e_page;
@@ -223,7 +258,7 @@ __global__ __launch_bounds__(512, 2) void prompt_kernel(const LatentShape sh, co
             qr[k][j] = __builtin_convertvector(__builtin_convertvector(*(const bf16x8*)(q + HD + 32 * j), f32x8) * down, bf16x8);
     }
     const int first_pos = t.first_pos + min(32 * wave, t.n_rows - 1), last_pos = t.first_pos + min(32 * wave + 31, t.n_rows - 1);  // of this wave's rows
-    const bool idle = 32 * wave >= t.n_rows;
+    const bool idle = 32 * wave >= t.n_rows, few = a.lse && first_pos < kLowPositions;
     int some = 0;  // pages in bf16 among those of this tile?
     {
         const int* format = a.format + (int64_t)hl * a.n_chunks * 2;
@@ -280,6 +315,28 @@ __global__ __launch_bounds__(512, 2) void prompt_kernel(const LatentShape sh, co
                 const bf16x8 kf = *(const bf16x8*)(sm.r[b][p] + (4 * j + g) * 128 + n * 8);
 #pragma unroll
                 for (int k = 0; k < NT; ++k) s[p][k] = mfma16(kf, qr[k][j], s[p][k]);
+            }
+        }
+        if (few && 16 * vp0 < kLowPositions + 16) {
+#pragma unroll 1
+            for (int p = 0; p < 4; ++p) {
+                const int low = vp0 + p < t.page_end ? ((scalar_row)a.e_low)[expanded(vp0 + p)] : -1;
+                if (low < 0) continue;
+                const _Float16* from = (const _Float16*)a.k_low + ((int64_t)hl * a.n_low + low) * (16 * HD) + g * 128 + n * 8;
+                f32x4 rest[NT];
+#pragma unroll
+                for (int k = 0; k < NT; ++k) rest[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < KS; ++j) {
+                    const f16x8 kf = *(const f16x8*)(from + j * 512);
+#pragma unroll
+                    for (int k = 0; k < NT; ++k) rest[k] = mfma16(kf, qf[k][j], rest[k]);
+                }
+#pragma unroll
+                for (int x = 0; x < 4; ++x)  // (s is indexed by the unrolled x)
+                    if (x == p)
+#pragma unroll
+                        for (int k = 0; k < NT; ++k) s[x][k] += rest[k] * 0x1p-11f;
             }
         }
         // pages that hold tokens ahead of some row, none at all, or the end of a prefix

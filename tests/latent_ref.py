@@ -110,6 +110,7 @@ def attention(batch, q, w, tok, H, R, hd, scale, absorbed):
             z = p.sum(1, keepdims=True)
             p /= z
             out[rows, h], lse[rows, h] = p @ v, (m + np.log(z))[:, 0]
+            D = np.minimum(D, 300)  # (the bound is without effect long before)
             off = np.expm1(2 * D) + U
             bound = off * (p @ np.abs(v))
             if absorbed:

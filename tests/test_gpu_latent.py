@@ -140,3 +140,48 @@ def test_append_writes_its_slots_and_nothing_else(n, R, wide):
     keep = (slots >= 0) & (slots < n_pages * 16)
     before[slots[keep]] = rows[keep][:, -(R + ROPE):]
     assert np.array_equal(rows_of(pages.float().cpu().numpy()), before)
+
+
+@pytest.mark.parametrize("H,R,hd", [(16, 512, 128), (5, 256, 64)])
+def test_the_normaliser_of_short_contexts_is_as_exact_as_its_type(H, R, hd):
+    """lse is fp32, whatever the operands are: rounded queries (decode) and keys (prompts) must not be seen in it.  2-norm over all rows:
+    first-order effects are taken out, so that what is left is U^2 of a score (1.5e-5 of 1, averaged over the row's tokens) in a decode
+    step, and for prompts 2^-11 of a key (3e-4 of a score of 1, over the square root of 128 tokens and more) for rows that see many,
+    against values of 1 to 6."""
+    requests = [(0, [[n]]) for n in (1, 2, 3, 5, 9, 17, 33, 40)] + [(19, [[3], [30]]), (5, [[1], [180]])]
+    b = Batch(requests, 21, new=[1, 2, 3, 5, 9, 17, 33, 2, 3, 30, 1, 100])
+    q, w, tok = values(b, H, R, hd, 22)
+    want = attention(b, q, w, tok, H, R, hd, (hd + ROPE) ** -0.5, False)
+    got = run(context(H, R, hd), b, q, w, tok, True)
+    check(got, want, "short prompts")
+    assert np.linalg.norm(got[1] - want[1]) <= 1e-5 * np.linalg.norm(want[1])
+    b.new[:] = 1
+    q = q[:b.S]
+    want = attention(b, q, w, tok, H, R, hd, (hd + ROPE) ** -0.5, True)
+    got = run(context(H, R, hd), b, q, w, tok)
+    check(got, want, "short decode")
+    assert np.linalg.norm(got[1] - want[1]) <= 1e-5 * np.linalg.norm(want[1])
+
+
+@pytest.mark.parametrize("factor", [2.0 ** 18, 2.0 ** -16])
+def test_prompts_whose_keys_and_values_half_precision_does_not_hold(factor):
+    """Some tokens' latents far larger or smaller than half precision (the queries see to it that the scores stay of order one)."""
+    H, R, hd = 8, 512, 128
+    b = Batch([(70, [[90], [20]]), (0, [[150]])], 31, new=[40, 20, 150])
+    q, w, tok = values(b, H, R, hd, 32)
+    q[..., :hd] /= np.float32(factor)
+    some = np.concatenate([b.slots(0)[:40], b.slots(2)])
+    tok[some, :R] *= np.float32(factor)
+    want = attention(b, q, w, tok, H, R, hd, (hd + ROPE) ** -0.5, False)
+    out, lse = run(context(H, R, hd), b, q, w, tok, True)
+    err = np.abs(out - want[0])
+    assert (err <= want[2] + 0 * err).all() and (np.abs(lse - want[1]) <= want[3]).all()
+    for rows in (slice(0, 60), slice(60, 210)):  # (their sizes differ by the factor)
+        assert np.sqrt(np.mean(err[rows] ** 2)) <= RMS * np.sqrt(np.mean(want[0][rows] ** 2))
+
+
+def test_few_new_tokens_behind_a_long_context_are_cut_into_pieces():
+    H, R, hd = 4, 512, 128
+    b = Batch([(0, [[3000]]), (1100, [[500], [3]])], 41, new=[20, 300, 3])
+    q, w, tok = values(b, H, R, hd, 42)
+    check(run(context(H, R, hd), b, q, w, tok, True), attention(b, q, w, tok, H, R, hd, (hd + ROPE) ** -0.5, False), "pieces")
