@@ -185,3 +185,203 @@ def test_few_new_tokens_behind_a_long_context_are_cut_into_pieces():
     b = Batch([(0, [[3000]]), (1100, [[500], [3]])], 41, new=[20, 300, 3])
     q, w, tok = values(b, H, R, hd, 42)
     check(run(context(H, R, hd), b, q, w, tok, True), attention(b, q, w, tok, H, R, hd, (hd + ROPE) ** -0.5, False), "pieces")
+
+
+def setup(seed, H=16, R=512, hd=128, requests=None, new=None):
+    import torch
+    b = Batch(requests or [(150, [[10], [70]]), (0, [[333]])], seed, new=new)
+    q, w, tok = values(b, H, R, hd, seed + 1)
+    d = dict(b=b, host=(q, w, tok), q=dev(q), w=dev(w), pages=dev(pool_of(tok)),
+             out=torch.zeros(q.shape[0], H, hd, dtype=torch.bfloat16, device="cuda:0"), lse=torch.zeros(q.shape[0], H, device="cuda:0"))
+    return d
+
+
+@pytest.mark.parametrize("prompt", [False, True])
+def test_recorded_calls_replay_beside_eager_ones(prompt):
+    """Two plans of one context in two graphs, replayed with new inputs, other plans and eager calls in between."""
+    import torch
+    ctx = context(16, 512, 128)
+    new = [10, 33, 200] if prompt else None
+    one, two = setup(1, new=new), setup(5, new=new)
+    call = ctx.prompt_attention if prompt else ctx.decode_step_attention
+    graphs = []
+    side = torch.cuda.Stream()
+    for d in (one, two):
+        d["plan"] = plan_of(ctx, d["b"], prompt)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            call(d["plan"], d["q"], d["w"], d["pages"], d["out"], d["lse"])
+        graphs.append(g)
+    for round_ in range(4):
+        for d, g in zip((one, two), graphs):
+            d["q"].copy_(dev(to_bf16(np.random.default_rng(round_).standard_normal(tuple(d["q"].shape)))))
+            d["out"].zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            got = d["out"].clone(), d["lse"].clone()
+            extra = plan_of(ctx, d["b"], prompt)  # (a plan of its own for the eager call)
+            d["out"].zero_()
+            call(extra, d["q"], d["w"], d["pages"], d["out"], d["lse"])
+            torch.cuda.synchronize()
+            assert torch.equal(got[0], d["out"]) and torch.equal(got[1], d["lse"]) and d["out"].float().abs().sum() > 0
+            extra.free()
+
+
+def test_calls_on_another_stream_and_without_lse():
+    import torch
+    ctx, s = context(16, 512, 128), torch.cuda.Stream()
+    d = setup(9)
+    plan = plan_of(ctx, d["b"])
+    ctx.decode_step_attention(plan, d["q"], d["w"], d["pages"], d["out"], d["lse"])
+    torch.cuda.synchronize()
+    first = d["out"].clone()
+    with torch.cuda.stream(s):
+        d["out"].zero_()
+        ctx.decode_step_attention(plan, d["q"], d["w"], d["pages"], d["out"])
+    s.synchronize()
+    assert torch.equal(first, d["out"])
+    s.wait_stream(torch.cuda.current_stream())
+    ctx.decode_step_attention(plan, d["q"], d["w"], d["pages"], d["out"], stream=s)
+    s.synchronize()
+    assert torch.equal(first, d["out"])
+
+
+def test_freed_plans_hand_their_memory_on():
+    import torch
+    ctx = context(16, 512, 128)
+    for n in range(6):
+        d = setup(30 + n, requests=[(0, [[100 + 300 * (n % 3)]]), (20 * n, [[1], [2]])])
+        plan = plan_of(ctx, d["b"])
+        ctx.decode_step_attention(plan, d["q"], d["w"], d["pages"], d["out"], d["lse"])
+        plan.free()
+        torch.cuda.synchronize()
+        want = attention(d["b"], *d["host"], 16, 512, 128, 192 ** -0.5, True)
+        assert (np.abs(d["out"].double().cpu().numpy() - want[0]) <= want[2]).all()
+
+
+def test_tensors_that_do_not_fit_are_refused():
+    import torch
+    from paper_2605_06914_amd import TAPER_EINVAL, TaperError
+    ctx, d = context(16, 512, 128), setup(9)
+    plan = plan_of(ctx, d["b"])
+    good = dict(q=d["q"], w_up=d["w"], pages=d["pages"], out=d["out"], lse=d["lse"])
+    for name, bad in [("q", d["q"][:-1]), ("q", d["q"].float()), ("q", d["q"].cpu()), ("q", d["q"].transpose(0, 1)), ("w_up", d["w"][:, 1:].contiguous()),
+                      ("pages", d["pages"][1:]), ("out", d["out"][:, :15].contiguous()), ("lse", d["lse"].double()), ("lse", d["lse"][:2]),
+                      ("q", torch.empty(d["q"].numel() + 1, dtype=torch.bfloat16, device="cuda:0")[1:])]:
+        with pytest.raises(TaperError) as e:
+            ctx.decode_step_attention(plan, **dict(good, **{name: bad}))
+        assert e.value.status == TAPER_EINVAL, name
+    n = 8
+    rows = torch.zeros(n, 576, dtype=torch.bfloat16, device="cuda:0")
+    slots = torch.zeros(n, dtype=torch.int64, device="cuda:0")
+    pages = d["pages"]
+    for latent, rope, s in [(rows[:, :511], rows[:, 512:], slots), (rows[:7, :512], rows[:, 512:], slots), (rows[:, :512].float(), rows[:, 512:], slots),
+                            (rows[:, :512], rows[:, 511:575], slots), (rows[:, :512], rows[:, 512:], slots.int()),
+                            (torch.zeros(512, n, dtype=torch.bfloat16, device="cuda:0").t(), rows[:, 512:], slots)]:
+        with pytest.raises(TaperError) as e:
+            ctx.append(latent, rope, s, pages, d["b"].n_pages)
+        assert e.value.status == TAPER_EINVAL
+
+
+def test_a_request_from_its_prompt_through_branches_and_their_join():
+    """As an engine uses them together: pages from a pool, a prompt in two chunks, a fork in mid-page, branches that decode for some
+    steps, their join into one prefix, compaction of the pool, a step of the joined request; each attention against the definition."""
+    import torch
+    from paper_2605_06914_amd import PageMover, PagePool, append_slots, remap_pages
+    H, R, hd, layers = 16, 512, 128, 2
+    rng = np.random.default_rng(77)
+    n_pages = 64
+    pool, ctx, mover = PagePool(n_pages), context(H, R, hd), PageMover.latent(R, device=0)
+    pool.alloc(7)
+    pools = [torch.full((n_pages, 72, 16, 8), float("nan"), dtype=torch.bfloat16, device="cuda:0") for _ in range(layers)]
+    w = to_bf16(rng.standard_normal((H, 2 * hd, R)) * R ** -0.5)
+    w_d = dev(w)
+    tokens = [dict() for _ in range(layers)]  # what each branch has seen: per layer, branch -> [values of its tokens]
+
+    def fresh(n):
+        return to_bf16(rng.standard_normal((layers, n, R + ROPE)))
+
+    def put(rows, slots):
+        for l in range(layers):
+            x = dev(rows[l])
+            ctx.append(x[:, :R], x[:, R:], dev(np.asarray(slots, np.int64)), pools[l], n_pages)
+
+    def compare(q, out, seen):
+        """q, out of some rows; seen: per row the tokens it sees."""
+        for r in range(len(q)):
+            c = seen[r].astype(np.float64)
+            for h in range(0, H, 5):
+                k, v = c[:, :R] @ w[h, :hd].T.astype(np.float64), c[:, :R] @ w[h, hd:].T.astype(np.float64)
+                s = (k @ q[r, h, :hd] + c[:, R:] @ q[r, h, hd:]) * (hd + ROPE) ** -0.5
+                p = np.exp(s - s.max())
+                ref = p @ v / p.sum()
+                # (the same four roundings as elsewhere, bounded by their effect on scores of one: 6 U of the values' mean size)
+                assert np.abs(out[r, h] - ref).max() <= 6 * 2.0 ** -8 * np.sqrt((p ** 2 @ v ** 2) / p.sum() ** 2).max() * 4 + 2.0 ** -8 * np.abs(ref).max()
+
+    # the prompt: 90 tokens, in chunks of 50 and 40
+    row = np.zeros(0, np.int32)
+    prompt = fresh(90)
+    have = 0
+    for n in (50, 40):
+        row = np.concatenate([row, pool.alloc((have + n + 15) // 16 - len(row))])
+        t = np.arange(have, have + n)
+        put(prompt[:, have:have + n], row[t // 16].astype(np.int64) * 16 + t % 16)
+        have += n
+        plan = ctx.prompt_plan_build(row[None], [0], [0], [have], [n], n_pages)
+        for l in range(layers):
+            q = to_bf16(rng.standard_normal((n, H, hd + ROPE)))
+            out = torch.empty(n, H, hd, dtype=torch.bfloat16, device="cuda:0")
+            ctx.prompt_attention(plan, dev(q), w_d, pools[l], out)
+            some = [0, n // 2, n - 1]
+            compare(q[some], out.double().cpu().numpy()[some], [prompt[l, :have - n + 1 + i] for i in some])
+        plan.free()
+    # two children fork after 85 tokens (in the middle of a page), each private from then on; 5 steps
+    rows, moves = [], []
+    for _ in range(2):
+        child, copy = pool.fork(row, 85)
+        rows.append(child)
+        moves.append(copy)
+    mover.copy(pools, [m[0] for m in moves], [m[1] for m in moves], n_pages)
+    pool.release(row)
+    # as branches of one request: 80 shared tokens on full pages, then 5 of the copied page and what they generate
+    own = [list(prompt[:, 80:85].transpose(1, 0, 2)) for _ in range(2)]
+    lens = [5, 5]
+    for step in range(5):
+        for i in range(2):
+            if lens[i] % 16 == 0:
+                rows[i] = np.concatenate([rows[i], pool.alloc(1)])
+        table = np.full((2, max(map(len, rows))), -1, np.int32)
+        for i in range(2):
+            table[i, :len(rows[i])] = rows[i]
+        slots, _ = append_slots(table, [80, 80], [0, 1, 2], lens, 16, n_pages)
+        x = fresh(2)
+        put(x, slots)
+        for i in range(2):
+            own[i].append(x[:, i])
+            lens[i] += 1
+        plan = ctx.plan_build(table, [0, 0], [80, 80], lens, n_pages)
+        for l in range(layers):
+            q = to_bf16(rng.standard_normal((2, H, hd + ROPE)))
+            out = torch.empty(2, H, hd, dtype=torch.bfloat16, device="cuda:0")
+            ctx.decode_step_attention(plan, dev(q), w_d, pools[l], out)
+            compare(q, out.double().cpu().numpy(), [np.concatenate([prompt[l, :80], np.stack([t[l] for t in own[i]])]) for i in range(2)])
+        plan.free()
+    # join: prefix, then both branches, one contiguous run; what was theirs is free again; the pool moves to its front
+    joined = np.concatenate([rows[0][:5], pool.alloc(2)])
+    src = np.concatenate([rows[0], rows[1][5:]])
+    mover.pack(pools, src[None], [80], [0, 2], lens, joined[None, 5:], n_pages, first_token=[80])
+    pool.share(joined[:5])
+    for r in rows:
+        pool.release(r)
+    pool.release(np.arange(7))
+    src, dst = pool.compact()
+    mover.copy(pools, src, dst, n_pages)
+    joined = remap_pages(joined, src, dst)
+    assert sorted(joined) == list(range(7)) and pool.free_pages == n_pages - 7
+    plan = ctx.plan_build(joined[None], [0], [100], [0], n_pages)
+    for l in range(layers):
+        q = to_bf16(rng.standard_normal((1, H, hd + ROPE)))
+        out = torch.empty(1, H, hd, dtype=torch.bfloat16, device="cuda:0")
+        ctx.decode_step_attention(plan, dev(q), w_d, pools[l], out)
+        compare(q, out.double().cpu().numpy(), [np.concatenate([prompt[l, :80], *[np.stack([t[l] for t in own[i]]) for i in range(2)]])])

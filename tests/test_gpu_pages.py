@@ -95,3 +95,50 @@ def test_pack(fmt, whole):
             r[dst[s, i // 16].astype(np.int64) * 16 + i % 16] = r[slots]
         got = back(t)
         assert np.array_equal(kv_rows(got, fmt[1], fmt[2]) if fmt[0] == "kv" else rows_of(got), r)
+
+
+def test_recorded_copies_replay_and_joins_are_not_recorded():
+    import torch
+    from paper_2605_06914_amd import TAPER_EINVAL, TaperError
+    fmt, n = ("kv", 1, 64), 600
+    rng = np.random.default_rng(5)
+    mover = mover_of(fmt)
+    ids = rng.permutation(2 * n + 2).astype(np.int32)
+    _, pools = make_pools(fmt, 2 * n + 2, 2, 6)
+    dev = on_device(pools)
+    side, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        mover.copy(dev, ids[:n], ids[n:2 * n], 2 * n + 2)
+        with pytest.raises(TaperError) as e:
+            mover.pack(dev, ids[None, :1], [5], [0, 0], [], ids[None, 1:2], 2 * n + 2)
+        assert e.value.status == TAPER_EINVAL
+    for r in range(3):
+        _, pools = make_pools(fmt, 2 * n + 2, 2, 10 + r)
+        for t, p in zip(dev, pools):
+            t.copy_(on_device([p])[0])
+        g.replay()
+        torch.cuda.synchronize()
+        for t, p in zip(dev, pools):
+            p[ids[n:2 * n]] = p[ids[:n]]
+            assert np.array_equal(back(t), p)
+        mover.copy(dev, ids[n:2 * n], ids[:n], 2 * n + 2)  # (eager, through the mover's own lists)
+        torch.cuda.synchronize()
+
+
+def test_many_calls_in_flight_on_two_streams():
+    """More calls than the mover has lists: each waits for the one whose list it takes."""
+    import torch
+    fmt, n = ("latent", 1, 320), 300
+    mover = mover_of(fmt)
+    _, a = make_pools(fmt, 2 * n, 1, 1)
+    _, c = make_pools(fmt, 2 * n, 1, 2)
+    dev = [on_device(a), on_device(c)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    rng = np.random.default_rng(3)
+    for i in range(24):
+        ids = rng.permutation(2 * n).astype(np.int32)
+        mover.copy(dev[i % 2], ids[:n], ids[n:], 2 * n, stream=streams[i % 2])
+        (a, c)[i % 2][0][ids[n:]] = (a, c)[i % 2][0][ids[:n]]
+    torch.cuda.synchronize()
+    assert np.array_equal(back(dev[0][0]), a[0]) and np.array_equal(back(dev[1][0]), c[0])

@@ -1,0 +1,146 @@
+"""Host side of the latent-cache operators: what a plan's items cover, and what is refused (no GPU)."""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+
+from paper_2605_06914_amd import (LATENT_EXPORTED, PAGES_EXPORTED, TAPER_EBLOCK, TAPER_EGROUP, TAPER_EHIP, TAPER_EINVAL, TAPER_ELEN, LatentContext,
+                                  TaperError, load_library)
+from tests.latent_ref import Batch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def test_library_exports_every_declared_symbol():
+    lib = load_library()
+    for header, macro, names in (("taper_latent.h", "TAPER_LATENT_API", LATENT_EXPORTED), ("taper_pages.h", "TAPER_PAGES_API", PAGES_EXPORTED)):
+        text = open(os.path.join(ROOT, "include", header)).read()
+        declared = set(re.findall(macro + r"\s+[\w\s\*]+?\b(taper_\w+)\s*\(", text))
+        assert declared == set(names), declared ^ set(names)
+        for n in names:
+            assert getattr(lib, n) is not None
+
+
+def host(H=16, R=512, hd=128, **kw):
+    return LatentContext(H, R, hd, device=-1, **kw)
+
+
+def refused(status, f, *a, **kw):
+    with pytest.raises(TaperError) as e:
+        f(*a, **kw)
+    assert e.value.status == status, e.value
+
+
+@pytest.mark.parametrize("bad", [dict(n_heads=0), dict(n_heads=257), dict(latent_dim=384), dict(head_dim=96), dict(rope_dim=32),
+                                 dict(page_size=32), dict(scale=0.0), dict(scale=float("nan")), dict(scale=float("inf"))])
+def test_create_rejects_unsupported_shapes(bad):
+    refused(TAPER_EINVAL, LatentContext, **dict(dict(n_heads=16, latent_dim=512, head_dim=128, device=-1), **bad))
+
+
+REQUESTS = [(0, [[1]]), (0, [[5000]]), (100, [[0], [17], [300]]), (64, [[5]] * 9), (33, [[16, 0, 40]]), (2000, [[n] for n in range(40)])]
+
+
+@pytest.mark.parametrize("H", [1, 5, 16, 64, 100, 128, 256])
+@pytest.mark.parametrize("workgroups", [0, 1, 30, 2000])
+def test_items_cover_every_token_of_every_row_once(H, workgroups):
+    b = Batch(REQUESTS, 1)
+    e = host(H).plan_build(b.table, b.group, b.prefix, b.seg_len, b.n_pages, target_workgroups=workgroups, seg_start=b.seg_start).export()
+    seen = [{h: [] for h in range(H)} for _ in range(b.S)]  # physical slots per row
+    rows_used = np.zeros(e["n_partial_rows"], int)
+    part_of = {}
+    assert len(e["items"]) % 8 == 0
+    for seq0, page0, n_tokens, row0, n_rows, part_row in e["items"]:
+        if n_rows == 0:
+            continue
+        assert 1 <= n_rows <= 64 and n_tokens >= 1
+        t = np.arange(n_tokens)
+        slots = b.table[seq0, page0 + t // 16].astype(np.int64) * 16 + t % 16
+        for r in range(n_rows):
+            s, h = divmod(row0 + r, H)
+            seen[s][h].append(slots)
+            rows_used[part_row + r] += 1
+            part_of.setdefault((s, h), []).append(part_row + r)
+    assert (rows_used == 1).all()
+    for s in range(b.S):
+        want = np.sort(b.slots(s))
+        for h in range(H):
+            assert np.array_equal(np.sort(np.concatenate(seen[s][h])), want), (s, h)
+        pieces = e["piece_row"][e["piece_start"][s]:e["piece_start"][s + 1]]
+        for h in range(H):
+            assert sorted(pieces + h) == sorted(part_of[s, h])
+    lengths = [sum(b.seg_len[b.seg_start[s]:b.seg_start[s + 1]]) for s in range(b.S)]
+    assert e["tokens_logical"] == sum(p + n for p, n in zip(b.prefix, lengths))
+    assert e["tokens_unique"] == sum(p for p, _ in REQUESTS) + sum(lengths)
+
+
+def test_a_long_context_is_not_cut_into_more_pieces_than_a_merge_should_read():
+    b = Batch([(0, [[32768]])], 1)
+    e = host(4).plan_build(b.table, b.group, b.prefix, b.seg_len, b.n_pages, target_workgroups=100000).export()
+    assert e["piece_start"][1] <= 64
+
+
+def test_plan_refusals_are_those_of_the_other_plans():
+    b = Batch([(40, [[3], [4]]), (0, [[20]])], 1)
+    ctx = host()
+
+    def build(**over):
+        a = dict(table=b.table.copy(), group=list(b.group), prefix=list(b.prefix), suffix=list(b.seg_len), n=b.n_pages)
+        a.update(over)
+        return ctx.plan_build(a["table"], a["group"], a["prefix"], a["suffix"], a["n"])
+
+    assert build().export()["n_seqs"] == 3
+    bad = b.table.copy()
+    bad[0, 0] = b.n_pages
+    refused(TAPER_EBLOCK, build, table=bad)
+    bad = b.table.copy()
+    bad[2, 1] = -1
+    refused(TAPER_EBLOCK, build, table=bad)
+    bad = b.table.copy()
+    bad[1, 0] = b.unreferenced[0]
+    refused(TAPER_EGROUP, build, table=bad)
+    refused(TAPER_EGROUP, build, group=[0, 0, 2])
+    refused(TAPER_EGROUP, build, prefix=[40, 41, 0])
+    refused(TAPER_ELEN, build, suffix=[3, -1, 20])
+    refused(TAPER_ELEN, build, suffix=[3, 4, 0])
+    refused(TAPER_ELEN, build, suffix=[3, 4, 2000])
+    refused(TAPER_EINVAL, build, suffix=[3, 4])
+    refused(TAPER_EINVAL, ctx.plan_build, b.table, b.group, b.prefix, b.seg_len, b.n_pages, seg_start=[0, 2, 1, 3])
+
+
+def test_prompt_plan_refusals():
+    b = Batch([(40, [[3], [4]]), (0, [[20]])], 1)
+    ctx = host()
+
+    def build(new):
+        return ctx.prompt_plan_build(b.table, b.group, b.prefix, b.seg_len, new, b.n_pages)
+
+    p = build([3, 0, 20])
+    assert p.prompt and p.n_rows == 23
+    refused(TAPER_ELEN, build, [4, 0, 20])
+    refused(TAPER_ELEN, build, [3, -1, 20])
+    refused(TAPER_ELEN, build, [0, 0, 0])
+    refused(TAPER_EINVAL, build, [3, 0])
+    refused(TAPER_EINVAL, p.export)
+
+
+def test_calls_without_a_device_or_with_another_plan_are_refused():
+    lib = load_library()
+    b = Batch([(0, [[20]])], 1)
+    ctx, other = host(), host()
+    plan = ctx.plan_build(b.table, b.group, b.prefix, b.seg_len, b.n_pages)
+    prompt = ctx.prompt_plan_build(b.table, b.group, b.prefix, b.seg_len, [5], b.n_pages)
+    any_ptr = ctypes.c_void_p(4096)
+    call = lib.taper_latent_decode_step_attention
+    assert call(ctx._h, plan._h, any_ptr, any_ptr, any_ptr, any_ptr, None, None) == TAPER_EHIP
+    assert call(other._h, plan._h, any_ptr, any_ptr, any_ptr, any_ptr, None, None) == TAPER_EINVAL
+    assert call(ctx._h, prompt._h, any_ptr, any_ptr, any_ptr, any_ptr, None, None) == TAPER_EINVAL
+    assert lib.taper_latent_prompt_attention(ctx._h, plan._h, any_ptr, any_ptr, any_ptr, any_ptr, None, None) == TAPER_EINVAL
+    assert call(ctx._h, None, any_ptr, any_ptr, any_ptr, any_ptr, None, None) == TAPER_EINVAL
+    append = lib.taper_latent_append
+    assert append(ctx._h, 4, any_ptr, 512, any_ptr, 64, any_ptr, any_ptr, 10, None) == TAPER_EHIP
+    assert append(ctx._h, -1, any_ptr, 512, any_ptr, 64, any_ptr, any_ptr, 10, None) == TAPER_EINVAL
+    assert append(ctx._h, 4, any_ptr, 511, any_ptr, 64, any_ptr, any_ptr, 10, None) == TAPER_EINVAL
+    assert append(ctx._h, 4, any_ptr, 520, any_ptr, 60, any_ptr, any_ptr, 10, None) == TAPER_EINVAL
+    assert append(ctx._h, 4, any_ptr, 512, any_ptr, 64, any_ptr, any_ptr, 0, None) == TAPER_EINVAL
