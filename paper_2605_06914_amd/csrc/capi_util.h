@@ -7,6 +7,7 @@
 #include <string>
 
 #include "taper_attn.h"
+#include "taper_plan.h"
 
 namespace taper {
 
@@ -53,6 +54,21 @@ int guarded(F&& f) {
     } catch (...) {
         return set_error(TAPER_EINVAL, "unexpected error");
     }
+}
+
+// What a batch's arrays say, checked as taper_plan_build_segments checks them: block table, lengths, page counts, segments and request
+// CSR of `out`.  (Its shares are for a single workgroup, which is the quickest; they are not used.)
+inline int resolve_batch(int page_size, int n_seqs, const int32_t* block_table, int bt_row_stride, const int32_t* branch_group,
+                         const int32_t* prefix_len, const int32_t* seg_start, const int32_t* seg_len, int64_t n_pool_pages, HostPlan* out) {
+    taper_attn_config one_head = {1, 1, 64, page_size, 1.0f, -1, TAPER_PARTIAL_F16_SCALED};
+    taper_plan_options o = {};
+    o.target_workgroups = 1;
+    o.share_prefix = 1;
+    o.pool_pct = o.solo_item_tokens = o.small_step_grid = -1;
+    std::string err;
+    const int st = build_host_plan_segments(one_head, n_seqs, block_table, bt_row_stride, branch_group, prefix_len, seg_start, seg_len,
+                                            n_pool_pages, &o, out, &err);
+    return st == TAPER_OK ? st : set_error(st, err);
 }
 
 }  // namespace taper

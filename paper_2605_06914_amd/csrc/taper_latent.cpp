@@ -227,14 +227,10 @@ void make_decode_items(const taper_latent_config& cfg, int units, taper_latent_p
     std::vector<Span> spans;
     for (int g = 0; g < b.n_groups; ++g) {
         const int s0 = b.group_start[g], s1 = b.group_start[g + 1];
-        plan->batch.tokens_unique += b.prefix_len[s0];
         if (b.prefix_len[s0] > 0) spans.push_back({s0, 0, b.prefix_len[s0], s0 * H, (s1 - s0) * H});
         for (int s = s0; s < s1; ++s)
             for (int k = b.seg_start[s]; k < b.seg_start[s + 1]; ++k)
-                if (b.seg_len[k] > 0) {
-                    spans.push_back({s, b.seg_page0[k], b.seg_len[k], s * H, H});
-                    plan->batch.tokens_unique += b.seg_len[k];
-                }
+                if (b.seg_len[k] > 0) spans.push_back({s, b.seg_page0[k], b.seg_len[k], s * H, H});
     }
     double total = 0;
     for (const Span& s : spans) {
@@ -271,15 +267,14 @@ int build_decode(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, 
                  const int32_t* seg_start, const int32_t* seg_len, int64_t n_pool_pages, int target_workgroups, hipStream_t s,
                  taper_latent_plan* plan) {
     const taper_latent_config& cfg = ctx->cfg;
-    std::string err;
     std::vector<int32_t> one;
     if (!seg_start && n_seqs > 0) {
         one.resize((size_t)n_seqs + 1);
         for (int i = 0; i <= n_seqs; ++i) one[i] = i;
         seg_start = one.data();
     }
-    const int st = taper::resolve_batch(cfg.page_size, n_seqs, block_table, stride, group, prefix, seg_start, seg_len, n_pool_pages, &plan->batch, &err);
-    if (st != TAPER_OK) return set_error(st, err);
+    const int st = taper::resolve_batch(cfg.page_size, n_seqs, block_table, stride, group, prefix, seg_start, seg_len, n_pool_pages, &plan->batch);
+    if (st != TAPER_OK) return st;
     if ((int64_t)n_seqs * cfg.n_heads > INT32_MAX / 2) return set_error(TAPER_EINVAL, "too many query rows");
     make_decode_items(cfg, target_workgroups > 0 ? target_workgroups : ctx->units, plan);
     if (plan->n_partial_rows > INT32_MAX || plan->items.size() > kMostBlocks) return set_error(TAPER_EINVAL, "too many query rows");
@@ -376,11 +371,10 @@ void make_prompt_items(int units, taper_latent_plan* plan) {
 int build_prompt(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, int stride, const int32_t* group, const int32_t* prefix,
                  const int32_t* suffix, const int32_t* new_len, int64_t n_pool_pages, hipStream_t s, taper_latent_plan* plan) {
     const taper_latent_config& cfg = ctx->cfg;
-    std::string err;
     std::vector<int32_t> one((size_t)n_seqs + 1);
     for (int i = 0; i <= n_seqs; ++i) one[i] = i;
-    const int st = taper::resolve_batch(cfg.page_size, n_seqs, block_table, stride, group, prefix, one.data(), suffix, n_pool_pages, &plan->batch, &err);
-    if (st != TAPER_OK) return set_error(st, err);
+    const int st = taper::resolve_batch(cfg.page_size, n_seqs, block_table, stride, group, prefix, one.data(), suffix, n_pool_pages, &plan->batch);
+    if (st != TAPER_OK) return st;
     const taper::HostPlan& b = plan->batch;
     const int P = cfg.page_size;
     plan->prompt = true;

@@ -355,9 +355,8 @@ int taper_pages_pack(taper_mover* m, int n_layers, void* const* pools, int n_seq
         std::vector<int32_t> group((size_t)n_seqs);
         for (int q = 0; q < n_seqs; ++q) group[q] = q;  // every sequence for itself
         taper::HostPlan b;
-        std::string err;
-        int st = taper::resolve_batch(P, n_seqs, block_table, bt_row_stride, group.data(), prefix_len, seg_start, seg_len, n_pool_pages, &b, &err);
-        if (st != TAPER_OK) return set_error(st, err);
+        int st = taper::resolve_batch(P, n_seqs, block_table, bt_row_stride, group.data(), prefix_len, seg_start, seg_len, n_pool_pages, &b);
+        if (st != TAPER_OK) return st;
         std::vector<taper::PackPage> pages;
         std::vector<int32_t> run_start(1, 0), run_token, run_entry;
         for (int q = 0; q < n_seqs; ++q) {

@@ -463,9 +463,12 @@ int build_host_plan(const taper_attn_config& cfg, int n_seqs, const int32_t* blo
                                     suffix_len, n_pool_pages, opts, out, err);
 }
 
-int resolve_batch(int page_size, int n_seqs, const int32_t* block_table, int bt_row_stride, const int32_t* branch_group,
-                  const int32_t* prefix_len, const int32_t* seg_start, const int32_t* seg_len, int64_t n_pool_pages, HostPlan* out,
-                  std::string* err) {
+static int build_for_grid(const taper_attn_config& cfg, int n_seqs, const int32_t* block_table, int bt_row_stride,
+                          const int32_t* branch_group, const int32_t* prefix_len, const int32_t* seg_start,
+                          const int32_t* seg_len, int64_t n_pool_pages, const taper_plan_options* opts,
+                          HostPlan* out, std::string* err) {
+    int st = validate_config(cfg, err);
+    if (st != TAPER_OK) return st;
     if (!block_table || !branch_group || !prefix_len || !seg_start || !out) {
         *err = "null argument";
         return TAPER_EINVAL;
@@ -478,7 +481,19 @@ int resolve_batch(int page_size, int n_seqs, const int32_t* block_table, int bt_
         *err = "n_pool_pages exceeds the int32 page id range";
         return TAPER_EINVAL;
     }
-    const int P = page_size;
+    const int P = cfg.page_size;
+    const int g = cfg.n_q_heads / cfg.n_kv_heads;
+    int target_wgs = opts && opts->target_workgroups > 0 ? opts->target_workgroups : 512;
+    const bool share_prefix = opts ? opts->share_prefix != 0 : true;
+    // A shared item holds up to 12 row tiles.  At head_dim 64 requests are cut at 8 unless asked otherwise: a line from a kernel
+    // that ran only one workgroup of more per compute unit, which no longer holds (146 to 149 VGPRs, two workgroups).  One
+    // item of up to 12 tiles instead measures 79.6 us against 94.6 at 33 branches of 4 query heads, 93 against 99 at 40, 104 against
+    // 111 at 48; with 8 query heads 75 against 84 at 17 branches, but 80.8 against 78.4 at 20 and 83 against 81 at 24.
+    // 64: per-branch flags of the shared kernel.
+    const int hard_cap = std::min(64, std::max(2, kMaxRowTilesPerItem * 16 / g));
+    int cap_branches = std::min(hard_cap, std::max(2, (cfg.head_dim == 128 ? kMaxRowTilesPerItem : 8) * 16 / g));
+    if (opts && opts->max_branches_per_item > 0) cap_branches = std::max(1, std::min(hard_cap, opts->max_branches_per_item));
+
     HostPlan& p = *out;
     p = HostPlan();
     p.n_seqs = n_seqs;
@@ -583,30 +598,6 @@ int resolve_batch(int page_size, int n_seqs, const int32_t* block_table, int bt_
             }
         }
     }
-    return TAPER_OK;
-}
-
-static int build_for_grid(const taper_attn_config& cfg, int n_seqs, const int32_t* block_table, int bt_row_stride,
-                          const int32_t* branch_group, const int32_t* prefix_len, const int32_t* seg_start,
-                          const int32_t* seg_len, int64_t n_pool_pages, const taper_plan_options* opts,
-                          HostPlan* out, std::string* err) {
-    int st = validate_config(cfg, err);
-    if (st != TAPER_OK) return st;
-    const int g = cfg.n_q_heads / cfg.n_kv_heads;
-    int target_wgs = opts && opts->target_workgroups > 0 ? opts->target_workgroups : 512;
-    const bool share_prefix = opts ? opts->share_prefix != 0 : true;
-    // A shared item holds up to 12 row tiles.  At head_dim 64 requests are cut at 8 unless asked otherwise: a line from a kernel
-    // that ran only one workgroup of more per compute unit, which no longer holds (146 to 149 VGPRs, two workgroups).  One
-    // item of up to 12 tiles instead measures 79.6 us against 94.6 at 33 branches of 4 query heads, 93 against 99 at 40, 104 against
-    // 111 at 48; with 8 query heads 75 against 84 at 17 branches, but 80.8 against 78.4 at 20 and 83 against 81 at 24.
-    // 64: per-branch flags of the shared kernel.
-    const int hard_cap = std::min(64, std::max(2, kMaxRowTilesPerItem * 16 / g));
-    int cap_branches = std::min(hard_cap, std::max(2, (cfg.head_dim == 128 ? kMaxRowTilesPerItem : 8) * 16 / g));
-    if (opts && opts->max_branches_per_item > 0) cap_branches = std::max(1, std::min(hard_cap, opts->max_branches_per_item));
-
-    HostPlan& p = *out;
-    st = resolve_batch(cfg.page_size, n_seqs, block_table, bt_row_stride, branch_group, prefix_len, seg_start, seg_len, n_pool_pages, out, err);
-    if (st != TAPER_OK) return st;
 
     // ---- segments of KV to stream
     std::vector<Segment> shared, priv;

@@ -69,11 +69,6 @@ int build_host_plan_segments(const taper_attn_config& cfg, int n_seqs, const int
 
 int validate_config(const taper_attn_config& cfg, std::string* err);
 
-// What a batch's arrays say, checked: block table, lengths, page counts, segments and request CSR of `out`; no work items yet.
-int resolve_batch(int page_size, int n_seqs, const int32_t* block_table, int bt_row_stride, const int32_t* branch_group,
-                  const int32_t* prefix_len, const int32_t* seg_start, const int32_t* seg_len, int64_t n_pool_pages, HostPlan* out,
-                  std::string* err);
-
 void resolve_slots_host(const HostPlan& p, int page_size, int64_t* slots, int64_t stride);
 
 }  // namespace taper
