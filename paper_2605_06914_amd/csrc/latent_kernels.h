@@ -8,8 +8,8 @@
 
 namespace taper {
 
-constexpr int kLatentTileTokens = 64;  // tokens a workgroup of the decode kernel takes at a time: a page per wave
-constexpr int kLatentTileRows = 64;    // query rows it holds at most
+constexpr int kLatentTileTokens = 64;  // tokens a workgroup of the decode kernel takes at a time
+constexpr int kLatentTileRows = 128;   // query rows it holds at most
 constexpr int kRopeDim = 64;
 
 struct LatentShape {

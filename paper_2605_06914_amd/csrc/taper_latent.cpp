@@ -141,7 +141,7 @@ constexpr size_t kMostBlocks = (size_t)1 << 22;  // of a launch (which has fewer
 // What some tokens cost: their tiles, at the price of the rows they meet (measured: a tile of 16 rows takes 3.1 us when all units
 // stream from memory, one of 64 rows 2.6 us where the L2 has it, a little more than the former where it has not).
 constexpr int kTile = taper::kLatentTileTokens, kRows = taper::kLatentTileRows;
-double tile_cost(int rows) { return rows <= 16 ? 0.9 : rows <= 32 ? 0.95 : 1.1; }
+double tile_cost(int rows) { return rows <= 64 ? 1.0 : rows <= 96 ? 1.2 : 1.5; }
 constexpr double kItemCost = 3.0;  // of an item beside its tiles: its queries in, its partial rows out
 constexpr int kMostPieces = 64;    // of a segment, about: a row's pieces are merged by some lanes of one workgroup
 

@@ -74,223 +74,220 @@ __global__ __launch_bounds__(64) void absorb_kernel(const LatentShape sh, const 
 }
 
 // ---------------------------------------------------------------------------
-// The attention.  A workgroup of 8 waves holds up to 64 query rows and takes 64 tokens (4 pages) at a time through LDS.  For the
-// scores, S^T = C Q^T, a wave owns a page and half of the rows (its queries stay in registers: 32 rows x 576 values are 144 of
-// them); for the product with the values, O^T = C^T P^T, it owns R / 8 of their columns and all rows.  K and V are the same
-// bytes, and LDS delivers them twice and once to the workgroup instead of once to each wave.  What the waves exchange is P (bf16, in
-// the layout in which the score product leaves it and the value product wants it).  V's operand is columns of a token-major page:
+// The attention.  A workgroup of 4 waves, one on each SIMD, holds up to 128 query rows, 32 a wave, and takes 64 tokens (4 pages) at a
+// time through LDS.  A wave makes the scores of its rows, S^T = C Q^T, weighs them and adds the values, O^T = C^T P^T, by itself: its
+// queries (32 rows x 576 values: 144 registers) and accumulators (32 rows x 512 values: 256, the accumulation registers) stay with it,
+// the weights leave the score product in the layout that the value product takes them in, and waves meet once a tile.  K and V are
+// the same bytes; each wave reads them from LDS twice, 68 KiB for 272 products, which at 128 bytes a clock and 4 waves is as long as
+// the products take: what bounds a compute unit whose rows are many.  V's operand is columns of a token-major page:
 // ds_read_b64_tr_b16 reads 4 tokens x 16 columns transposed.
+// Bringing a tile to LDS blocks the waves that ask for it (1200 clocks for its 72 KiB from the L2, 2200 from memory), so many rows a
+// tile matter (a workgroup of 64 rows, whose waves shared the work by pages and columns, took 6300 clocks a tile), and waves without
+// rows bring the tiles of items that have fewer than 97.
 // ---------------------------------------------------------------------------
-constexpr int kDecodeWaves = 8;
+// Weights are taken relative to a row's reference, the largest score of some earlier tile, so that a tile's weights do not wait for its
+// maximum.  A score that is more than this above its reference (in log2; a first tile always is) makes the wave take new references.
+// Weights are then at most 2^6: a bf16 weight has 8 bits whatever its size, sums and accumulators are fp32.
+constexpr float kMostAbove = 6.f;
+
 template <int R>
 struct DecodeSmem {
-    // (the small ones first: an LDS access has 16 bits of offset, and addresses beyond it cost a register each)
-    f32x4 mx[kLatentTileRows];   // a row's maximum in each of the four pages
-    f32x4 sum[kLatentTileRows];
-    bf16x8 p[2][4][64];          // [pair of pages][row tile][lane]: a lane's 4 tokens of each page side by side, as the value product takes them
-    int higher[kDecodeWaves];    // whether a wave's scores need a new reference
-    unsigned sink[64];           // nobody reads it (see touch)
+    unsigned sink[64];  // nobody reads it (see touch)
     __bf16 tile[2][4][(R + kRopeDim) * 16];
 };
 
-// Weights are taken relative to a row's reference, the largest score of some earlier tile: waves that own different pages of a row can
-// then weigh their scores at once and meet once a tile, instead of meeting for each tile's maximum first.  A score that is more than
-// this above its reference (in log2; a first tile always is) makes all waves meet for new references and weigh the tile again.  Weights
-// are then at most 2^6: a bf16 weight has 8 bits whatever its size, sums and accumulators are fp32.
-constexpr float kMostAbove = 6.f;
-template <int R, int NT>  // NT row tiles of 16
+template <int R, bool FULL>  // FULL: all waves have rows
 DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const taper_latent_item& it, DecodeSmem<R>& sm) {
-    constexpr int KD = R + kRopeDim, JK = KD / 32, DT = R / 16 / kDecodeWaves, NS = (NT + 1) / 2;  // NS: row tiles of a wave's scores
+    constexpr int KD = R + kRopeDim, JK = KD / 32, DT = R / 16, PAGE = KD * 16, NT = 1;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-    const int pg = wave & 3, k0 = (wave >> 2) * NS;  // page and first row tile of this wave's scores
-    const bool scores = k0 < NT;
+    const int row0 = wave * 16 * NT, busy = (it.n_rows + 16 * NT - 1) / (16 * NT);  // this wave's first row; waves that have rows
     const scalar_row row = (scalar_row)(a.bt + (int64_t)it.seq0 * a.bt_stride + it.page0);
     const int last_page = (it.n_tokens + 15) / 16 - 1, n_tiles = (it.n_tokens + 63) / 64;
     const char* pages = (const char*)a.pages;
     const float c = sh.scale_log2e;
-    constexpr int LOADS = (R + kRopeDim) / 64;  // a wave brings half of its page, a KiB at a time
-    const unsigned half_bytes = (wave >> 2) * (R + kRopeDim) * 16;
 
-    auto page = [&](int t) { return pages + (int64_t)row[min(4 * t + pg, last_page)] * ((R + kRopeDim) * 32) + half_bytes; };  // (past the end: the last one)
-    // Brings a tile's lines into the L2 two tiles before its own loads: pages are scattered, and from memory a tile took longer than
-    // another tile's work (one tile ahead only, a tile of 64 rows took 8400 clocks, of which 3000 were waiting).
-    constexpr int LINES = (R + kRopeDim) / 8, TOUCHES = (LINES + 63) / 64;
+    auto page = [&](int t, int pg) { return pages + (int64_t)row[min(4 * t + pg, last_page)] * (PAGE * 2); };  // (past the end: the last one)
+    auto place = [&](int t, int pg) { return uniform(lds_address(sm.tile[t & 1][pg])); };
+    auto load = [&](const char* from, unsigned to, int i) { load_to_lds(from + i * 1024, lane * 16, to + i * 1024); };  // (scalar sums: one lane offset for all)
+    constexpr int LOADS = PAGE / 1024;  // of half a page
+    if (!FULL && wave >= busy) {  // bring the tiles
+        const int others = 8 - busy;
+        auto bring = [&](int t) {
+            for (int x = wave - busy; x < 8; x += others) {  // half pages
+                const char* from = page(t, x & 3) + (x >> 2) * PAGE;
+                const unsigned to = place(t, x & 3) + (x >> 2) * PAGE;
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) load(from, to, i);
+            }
+        };
+        bring(0);
+        for (int t = 0; t < n_tiles; ++t) {
+            wait_loads_and_meet<0>();
+            if (t + 1 < n_tiles) bring(t + 1);
+        }
+        return;
+    }
+    const int pg = wave & 3, half_bytes = (wave >> 2) * PAGE;  // where all waves have rows each brings half of a page
+    // and its lines into the L2 two tiles before that: pages are scattered, and from memory a tile takes longer than another's work
+    constexpr int LINES = PAGE / 128, TOUCHES = (LINES + 63) / 64;
     auto touch = [&](const char* from) {
 #pragma unroll
         for (int i = 0; i < TOUCHES; ++i) word_to_lds(from, min(64 * i + lane, LINES - 1) * 128, uniform(lds_address(sm.sink)));
     };
-    {
-        const char* from = page(0);
-        const unsigned to = uniform(lds_address(sm.tile[0][pg])) + half_bytes;
+    const char *next = page(1, pg) + half_bytes, *next2 = page(2, pg) + half_bytes;
+    if (FULL) {
+        const char* from = page(0, pg) + half_bytes;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) load_to_lds(from + i * 1024, lane * 16, to + i * 1024);  // (scalar sums: one lane offset for all)
+        for (int i = 0; i < LOADS; ++i) load(from, place(0, pg) + half_bytes, i);
+        touch(next2);
     }
-    const char *next = page(1), *next2 = page(2);
-    touch(next2);
-    bf16x8 qf[NS][JK];
+    bf16x8 qf[NT][JK];
 #pragma unroll
-    for (int k = 0; k < NS; ++k) {
-        const __bf16* q = (const __bf16*)a.q_lat + (int64_t)(it.row0 + min(16 * (k0 + k) + n, it.n_rows - 1)) * KD + 8 * g;
+    for (int k = 0; k < NT; ++k) {
+        const __bf16* q = (const __bf16*)a.q_lat + (int64_t)(it.row0 + min(row0 + 16 * k + n, it.n_rows - 1)) * KD + 8 * g;
 #pragma unroll
         for (int j = 0; j < JK; ++j) qf[k][j] = *(const bf16x8*)(q + 32 * j);
     }
     f32x4 O[NT][DT];
-    float m[NT], l[NS];  // running maxima of all rows; sums of this wave's page and rows
+    float m[NT], l[NT];
 #pragma unroll
     for (int k = 0; k < NT; ++k) {
         m[k] = -INFINITY;
+        l[k] = 0.f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) O[k][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-#pragma unroll
-    for (int k = 0; k < NS; ++k) l[k] = 0.f;
     auto step = [&](const int t, auto last) {
-        wait_loads_and_meet<TOUCHES>();  // tile t is here for all, and all are done with tile t - 1
+        if (FULL) wait_loads_and_meet<TOUCHES>();  // tile t is here for all, and all are done with tile t - 1
+        else wait_loads_and_meet<0>();
+        constexpr bool bring = !decltype(last)::value && FULL;
         const char* const from = next;
-        const unsigned to = uniform(lds_address(sm.tile[(t + 1) & 1][pg])) + half_bytes;
+        const unsigned to = place(t + 1, pg) + half_bytes;
         next = next2;
-        next2 = page(t + 3);
-        auto load = [&](int i) {  // (between other instructions: all at once they would hold up what follows)
-            if (!last && i < LOADS) load_to_lds(from + i * 1024, lane * 16, to + i * 1024);
-        };
-        __bf16* const mine = sm.tile[t & 1][pg];
-        const int valid = it.n_tokens - 64 * t - 16 * pg;  // of this wave's page
-        if (last && it.n_tokens - 64 * t < 64) {  // what follows the last token may be anything: zeros, so that its zero weight meets no NaN
-            for (int i = lane + (wave >> 2) * 64; i < KD / 8 * 16; i += 128)
-                if ((i & 15) >= valid) *(u32x4*)(mine + i * 8) = u32x4{0, 0, 0, 0};
-            meet();
-        }
-        f32x4 s[NS];
-        float sum[NS];
-        bool higher = false;
-        auto ref = [&](int k) { return NT == NS || wave < 4 ? m[k] : m[NT - NS + k]; };  // reference of this wave's rows
-        auto weigh = [&] {
-#pragma unroll
-            for (int k = 0; k < NS; ++k) {
-                f32x4 p;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = fast_exp2(fmaf(s[k][i], c, -ref(k)));
-                sum[k] = (p[0] + p[1]) + (p[2] + p[3]);
-                // (8 bits of each weight, whatever its size); 8 tokens of a lane from two pages lie together
-                ((bf16x4*)&sm.p[pg >> 1][k0 + k][lane])[pg & 1] = __builtin_convertvector(p, bf16x4);
+        next2 = page(t + 3, pg) + half_bytes;
+        const __bf16* const tile = sm.tile[t & 1][0];
+        if (last && it.n_tokens - 64 * t < 64) {
+            // What follows the last token may be anything: zeros, so that its zero weight meets no NaN.  (Every wave writes all of them before
+            // it reads any: nobody need wait for another.)
+            for (int pg = 0; pg < 4; ++pg) {
+                const int valid = it.n_tokens - 64 * t - 16 * pg;
+                if (valid >= 16) continue;
+                for (int i = lane; i < KD / 8 * 16; i += 64)
+                    if ((i & 15) >= valid) *(u32x4*)(sm.tile[t & 1][pg] + i * 8) = u32x4{0, 0, 0, 0};
             }
-        };
-        if (scores) {
-            constexpr int AHEAD = 3;
-            bf16x8 kf[AHEAD];
-            const __bf16* const k_at = mine + g * 128 + n * 8;
+        }
+        f32x4 s[4][NT];
+        constexpr int AHEAD = 2;  // steps of two pages' operands in flight
 #pragma unroll
-            for (int j = 0; j < AHEAD; ++j) kf[j] = *(const bf16x8*)(k_at + j * 512);
+        for (int half = 0; half < 2; ++half) {  // two pages at a time: twice as many chains of products
+            const __bf16* const k_at = tile + half * 2 * PAGE + g * 128 + n * 8;
+            bf16x8 kf[AHEAD][2];
 #pragma unroll
-            for (int k = 0; k < NS; ++k) s[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < AHEAD; ++j)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) kf[j][x] = *(const bf16x8*)(k_at + x * PAGE + j * 512);
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int k = 0; k < NT; ++k) s[2 * half + x][k] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int j = 0; j < JK; ++j) {
 #pragma unroll
-                for (int k = 0; k < NS; ++k) s[k] = mfma16(kf[j % AHEAD], qf[k][j], s[k]);
-                if (j + AHEAD < JK) kf[j % AHEAD] = *(const bf16x8*)(k_at + (j + AHEAD) * 512);
-                if (j % 2 == 1) load(j / 2);
+                for (int x = 0; x < 2; ++x) {
+#pragma unroll
+                    for (int k = 0; k < NT; ++k) s[2 * half + x][k] = mfma16(kf[j % AHEAD][x], qf[k][j], s[2 * half + x][k]);
+                    if (j + AHEAD < JK) kf[j % AHEAD][x] = *(const bf16x8*)(k_at + x * PAGE + (j + AHEAD) * 512);
+                }
+                if (bring && j % 4 == 1 && half * (LOADS + 1) / 2 + j / 4 < (half ? LOADS : (LOADS + 1) / 2)) load(from, to, half * (LOADS + 1) / 2 + j / 4);
                 __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int i = JK / 2; i < LOADS; ++i) load(i);
-#pragma unroll
-            for (int k = 0; k < NS; ++k) {
-                if (last && valid < 16)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[k][i] = 4 * g + i < valid ? s[k][i] : -INFINITY;
-                const float mx = max_lane_groups(max4(s[k]));
-                higher |= !(mx * c <= ref(k) + kMostAbove);
-                if (g == 0) ((float*)&sm.mx[16 * (k0 + k) + n])[pg] = mx;
-            }
-            weigh();
-        } else {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) load(i);
         }
-        if (!last) touch(next2);
-        if (lane == 0) sm.higher[wave] = 0;
-        if (__any(higher) && lane == 0) sm.higher[wave] = 1;
-        meet();
-        {
-            typedef int i32x4 __attribute__((ext_vector_type(4)));
-            const i32x4 x = ((const i32x4*)sm.higher)[0] | ((const i32x4*)sm.higher)[1];
-            if (uniform(x[0] | x[1] | x[2] | x[3])) {  // (all waves alike)
-                float alpha[NT];
+        if (bring) touch(next2);
+        bool higher = false;
 #pragma unroll
-                for (int k = 0; k < NT; ++k) {
-                    const float mn = max2(m[k], max4(sm.mx[16 * k + n]) * c);
-                    alpha[k] = fast_exp2(m[k] - mn);
-                    m[k] = mn;
+        for (int k = 0; k < NT; ++k) {
+            if (last)
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) O[k][d] *= alpha[k];
-                }
-                if (scores) {
+                for (int p = 0; p < 4; ++p)
 #pragma unroll
-                    for (int k = 0; k < NS; ++k) l[k] *= NT == NS || wave < 4 ? alpha[k] : alpha[NT - NS + k];
-                    weigh();
-                }
-                meet();
+                    for (int i = 0; i < 4; ++i) s[p][k][i] = 64 * t + 16 * p + 4 * g + i < it.n_tokens ? s[p][k][i] : -INFINITY;
+            const float mx = max2(max2(max4(s[0][k]), max4(s[1][k])), max2(max4(s[2][k]), max4(s[3][k])));
+            higher |= !(mx * c <= m[k] + kMostAbove);
+        }
+        if (__any(higher)) {
+#pragma unroll
+            for (int k = 0; k < NT; ++k) {
+                const float mx = max2(max2(max4(s[0][k]), max4(s[1][k])), max2(max4(s[2][k]), max4(s[3][k])));
+                const float mn = max2(m[k], max_lane_groups(mx) * c), alpha = fast_exp2(m[k] - mn);
+                m[k] = mn;
+                l[k] *= alpha;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) O[k][d] *= alpha;
             }
         }
-        if (scores)
+        bf16x4 pr[4][NT];
 #pragma unroll
-            for (int k = 0; k < NS; ++k) l[k] += sum[k];
-        const __bf16* const v_at = sm.tile[t & 1][0] + wave * DT * 256 + (lane >> 1 & 1) * 128 + (4 * g + (n >> 2)) * 8 + (lane & 1) * 4;
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int k = 0; k < NT; ++k) {
+                f32x4 w;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = fast_exp2(fmaf(s[p][k][i], c, -m[k]));
+                l[k] += (w[0] + w[1]) + (w[2] + w[3]);
+                pr[p][k] = __builtin_convertvector(w, bf16x4);  // (8 bits of each weight)
+            }
+        const __bf16* const v_at = tile + (lane >> 1 & 1) * 128 + (4 * g + (n >> 2)) * 8 + (lane & 1) * 4;
         auto columns = [&](int x) {  // 16 columns of 32 tokens; x: column group, then pair of pages
             typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
-            const __bf16* at = v_at + x / DT * 2 * (KD * 16) + x % DT * 256;
-            const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)at), v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + KD * 16));
+            const __bf16* at = v_at + x / DT * 2 * PAGE + x % DT * 256;
+            const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)at), v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + PAGE));
             return cat(__builtin_bit_cast(bf16x4, v0), __builtin_bit_cast(bf16x4, v1));
         };
-        bf16x8 pf[NT], vf[2] = {columns(0), columns(1)};
+        constexpr int V_AHEAD = 4;
+        bf16x8 vf[V_AHEAD];
+#pragma unroll
+        for (int x = 0; x < V_AHEAD; ++x) vf[x] = columns(x);
 #pragma unroll
         for (int x = 0; x < 2 * DT; ++x) {
-            if (x % DT == 0)
 #pragma unroll
-                for (int k = 0; k < NT; ++k) pf[k] = sm.p[x / DT][k][lane];
-#pragma unroll
-            for (int k = 0; k < NT; ++k) O[k][x % DT] = mfma16(vf[x % 2], pf[k], O[k][x % DT]);
-            if (x + 2 < 2 * DT) vf[x % 2] = columns(x + 2);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int k = 0; k < NT; ++k) O[k][x % DT] = mfma16(vf[x % V_AHEAD], cat(pr[x / DT * 2][k], pr[x / DT * 2 + 1][k]), O[k][x % DT]);
+            if (x + V_AHEAD < 2 * DT) vf[x % V_AHEAD] = columns(x + V_AHEAD);
+            if (x % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (else more is read ahead than there are registers for)
         }
     };
     for (int t = 0; t < n_tiles - 1; ++t) step(t, std::false_type());
     step(n_tiles - 1, std::true_type());
-    // a row's sum: over the lane groups, and over the waves' pages (and nothing in flight to LDS when the workgroup ends)
-    if (scores)
-#pragma unroll
-        for (int k = 0; k < NS; ++k) {
-            const float mine = sum_lane_groups(l[k]);
-            if (g == 0) ((float*)&sm.sum[16 * (k0 + k) + n])[pg] = mine;
-        }
-    wait_loads_and_meet<0>();
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing on its way to LDS when the workgroup ends)
 #pragma unroll
     for (int k = 0; k < NT; ++k) {
-        const int r = 16 * k + n;
+        const int r = row0 + 16 * k + n;
+        const float total = sum_lane_groups(l[k]), inv = 1.0f / total;
         if (r >= it.n_rows) continue;
-        const f32x4 of = sm.sum[r];
-        const float total = (of[0] + of[1]) + (of[2] + of[3]), inv = 1.0f / total;
         const int64_t at = it.part_row + r;
-        float most = 0.f;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-            O[k][d] *= inv;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(O[k][d][i]));
-        }
-        const int e = exponent_of(max_lane_groups(most));
         // the row travels divided by its own sum, in half precision after division by a power of two of each eighth of its columns that
         // brings their largest magnitude into [0.5, 1): off by 2^-12 of that, whatever the magnitude, and half the bytes of fp32 rows
         PartStats* const st = a.stats + at;
-        if (g == 0) st->exponent[wave] = (signed char)e;
-        if (wave == 0 && g == 0) {
+#pragma unroll
+        for (int e8 = 0; e8 < 8; ++e8) {
+            float most = 0.f;
+            f32x4 v[DT / 8];
+#pragma unroll
+            for (int d = 0; d < DT / 8; ++d) {
+                v[d] = O[k][e8 * (DT / 8) + d] * inv;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(v[d][i]));
+            }
+            const int e = exponent_of(max_lane_groups(most));
+            if (g == 0) st->exponent[e8] = (signed char)e;
+            const float down = __uint_as_float((unsigned)(127 - e) << 23);
+            _Float16* to = (_Float16*)a.part + at * R + e8 * (R / 8) + 4 * g;
+#pragma unroll
+            for (int d = 0; d < DT / 8; ++d) *(f16x4*)(to + 16 * d) = __builtin_convertvector(v[d] * down, f16x4);
+        }
+        if (g == 0) {
             st->m = m[k];
             st->l = total;
         }
-        _Float16* to = (_Float16*)a.part + at * R + wave * (R / kDecodeWaves) + 4 * g;
-        const float down = __uint_as_float((unsigned)(127 - e) << 23);
-#pragma unroll
-        for (int d = 0; d < DT; ++d) *(f16x4*)(to + 16 * d) = __builtin_convertvector(O[k][d] * down, f16x4);
     }
 }
 
@@ -299,9 +296,8 @@ __global__ __launch_bounds__(512, 2) void latent_decode_kernel(const LatentShape
     __shared__ DecodeSmem<R> sm;
     const taper_latent_item it = a.items[blockIdx.x];
     if (it.n_rows <= 0) return;
-    if (it.n_rows <= 16) decode_item<R, 1>(sh, a, it, sm);
-    else if (it.n_rows <= 32) decode_item<R, 2>(sh, a, it, sm);
-    else decode_item<R, 4>(sh, a, it, sm);
+    if (it.n_rows <= 112) decode_item<R, false>(sh, a, it, sm);
+    else decode_item<R, true>(sh, a, it, sm);
 }
 
 // ---------------------------------------------------------------------------
@@ -325,7 +321,7 @@ __global__ __launch_bounds__(512) void finish_kernel(const LatentShape sh, const
         for (int j = 0; j < R / 32; ++j) wf[j] = *(const bf16x8*)(w + 32 * j);
     {
         constexpr int THREADS = 512 / SB, LANES = THREADS < 64 ? THREADS : 64;
-        const int i = tid / THREADS, d0 = tid % THREADS * PER, s = s0 + i, chunk = d0 / (R / kDecodeWaves);
+        const int i = tid / THREADS, d0 = tid % THREADS * PER, s = s0 + i, chunk = d0 / (R / 8);
         float acc[PER], M = -INFINITY, L = 0.f;
 #pragma unroll
         for (int j = 0; j < PER; ++j) acc[j] = 0.f;
@@ -445,8 +441,8 @@ hipError_t launch_latent_decode(const LatentShape& sh, const LatentDecodeArgs& a
     const dim3 grid(sh.n_heads, sh.latent_dim / 128, (a.n_seqs + s_per_block - 1) / s_per_block);
     if (sh.head_dim == 128) hipLaunchKernelGGL((absorb_kernel<4>), grid, dim3(64), 0, s, sh, a, s_per_block);
     else hipLaunchKernelGGL((absorb_kernel<2>), grid, dim3(64), 0, s, sh, a, s_per_block);
-    if (sh.latent_dim == 512) hipLaunchKernelGGL((latent_decode_kernel<512>), dim3(a.n_items), dim3(64 * kDecodeWaves), 0, s, sh, a);
-    else hipLaunchKernelGGL((latent_decode_kernel<256>), dim3(a.n_items), dim3(64 * kDecodeWaves), 0, s, sh, a);
+    if (sh.latent_dim == 512) hipLaunchKernelGGL((latent_decode_kernel<512>), dim3(a.n_items), dim3(512), 0, s, sh, a);
+    else hipLaunchKernelGGL((latent_decode_kernel<256>), dim3(a.n_items), dim3(512), 0, s, sh, a);
     // Sixteen sequences a workgroup read W_v once for all of them; where that leaves most of the chip idle, four.
     const bool many = (int64_t)sh.n_heads * ((a.n_seqs + 15) / 16) >= 256;
     if (sh.latent_dim == 512 && sh.head_dim == 128) launch_finish<512, 128>(many, sh, a, s);

@@ -54,7 +54,7 @@ def test_items_cover_every_token_of_every_row_once(H, workgroups):
     for seq0, page0, n_tokens, row0, n_rows, part_row in e["items"]:
         if n_rows == 0:
             continue
-        assert 1 <= n_rows <= 64 and n_tokens >= 1
+        assert 1 <= n_rows <= 128 and n_tokens >= 1
         t = np.arange(n_tokens)
         slots = b.table[seq0, page0 + t // 16].astype(np.int64) * 16 + t % 16
         for r in range(n_rows):
