@@ -142,7 +142,8 @@ constexpr size_t kMostBlocks = (size_t)1 << 22;  // of a launch (which has fewer
 // stream from memory, one of 64 rows 2.6 us where the L2 has it, a little more than the former where it has not).
 constexpr int kTile = taper::kLatentTileTokens, kRows = taper::kLatentTileRows;
 double tile_cost(int rows) { return rows <= 64 ? 1.0 : rows <= 96 ? 1.2 : 1.5; }
-constexpr double kItemCost = 3.0;  // of an item beside its tiles: its queries in, its partial rows out
+// of an item beside its tiles: its first tile's way from memory, its queries in, its partial rows out
+double start_cost(int rows) { return 2.5 + rows * (2.0 / 128); }
 constexpr int kMostPieces = 64;    // of a segment, about: a row's pieces are merged by some lanes of one workgroup
 
 struct Span {
@@ -167,7 +168,7 @@ struct DecodeItems {
     double time = 0;  // when the last unit ends, in tiles
 };
 
-double item_cost(const taper_latent_item& it) { return (it.n_tokens + kTile - 1) / kTile * tile_cost(it.n_rows) + kItemCost; }
+double item_cost(const taper_latent_item& it) { return (it.n_tokens + kTile - 1) / kTile * tile_cost(it.n_rows) + start_cost(it.n_rows); }
 
 void cut_spans(const std::vector<Span>& spans, int page_size, int units, double total, const CutRule& rule, DecodeItems* out) {
     struct Unit {
@@ -175,10 +176,10 @@ void cut_spans(const std::vector<Span>& spans, int page_size, int units, double 
         int first, n;
     };
     std::vector<Unit> stretches;
-    const double share = std::max(2.0 + kItemCost, total / units * rule.big);
+    const double share = total / units * rule.big;
     for (const Span& s : spans) {
         const int tiles = (s.n_tokens + kTile - 1) / kTile, least = std::max(1, tiles * 2 / kMostPieces);
-        const int big = std::max(least, (int)((share - kItemCost) / tile_cost(std::min(s.n_rows, kRows))));
+        const int widest = std::min(s.n_rows, kRows), big = std::max({least, 2, (int)((share - start_cost(widest)) / tile_cost(widest))});
         int t = 0, n_small = 0;
         if (tiles > big && rule.small_part > 1) n_small = std::max(std::max(least, big / rule.small_part), (int)(tiles * rule.small_share));
         while (t < tiles) {
@@ -236,7 +237,7 @@ void make_decode_items(const taper_latent_config& cfg, int units, taper_latent_p
     for (const Span& s : spans) {
         const int full = s.n_rows / kRows, rest = s.n_rows % kRows;
         const double each = full * tile_cost(kRows) + (rest ? tile_cost(rest) : 0.0);
-        total += (s.n_tokens + kTile - 1) / kTile * each + kItemCost * (full + (rest > 0));
+        total += (s.n_tokens + kTile - 1) / kTile * each + full * start_cost(kRows) + (rest ? start_cost(rest) : 0.0);
     }
     DecodeItems best;
     for (const CutRule& rule : kCutRules) {

@@ -22,7 +22,8 @@ template <int KS>  // head_dim / 32
 __global__ __launch_bounds__(64) void absorb_kernel(const LatentShape sh, const LatentDecodeArgs a, const int s_per_block) {
     const int lane = threadIdx.x, n = lane & 15, g = lane >> 4, h = blockIdx.x, r0 = blockIdx.y * 128;
     const int R = sh.latent_dim, KD = R + kRopeDim, HD = 32 * KS, H = sh.n_heads;
-    const __bf16* w = (const __bf16*)a.w_up + (int64_t)h * 2 * HD * R + r0 + 8 * n;
+    // lane n's columns are block 4 (n mod 4) + n / 4 of eight: a query's results then leave as 64 bytes in a row from four lanes
+    const __bf16* w = (const __bf16*)a.w_up + (int64_t)h * 2 * HD * R + r0 + 8 * ((n & 3) * 4 + (n >> 2));
     bf16x8 wf[KS][8];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
@@ -59,11 +60,11 @@ __global__ __launch_bounds__(64) void absorb_kernel(const LatentShape sh, const 
             bf16x8 v;
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = (__bf16)acc[i][j];
-            *(bf16x8*)(to + r0 + 8 * (4 * g + j)) = v;
+            *(bf16x8*)(to + r0 + 8 * (4 * j + g)) = v;
             if (a.lse) {  // what the rounding took away: finish_kernel puts its effect on the normaliser back
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = (__bf16)(acc[i][j] - (float)v[i]);
-                *(bf16x8*)((__bf16*)a.q_rest + ((int64_t)s * H + h) * R + r0 + 8 * (4 * g + j)) = v;
+                *(bf16x8*)((__bf16*)a.q_rest + ((int64_t)s * H + h) * R + r0 + 8 * (4 * j + g)) = v;
             }
         }
         if (r0 == 0) {
@@ -315,10 +316,11 @@ __global__ __launch_bounds__(512) void finish_kernel(const LatentShape sh, const
     const int H = sh.n_heads;
     constexpr int VT = HD / 16;  // waves with a tile of 16 values
     const __bf16* w = (const __bf16*)a.w_up + ((int64_t)h * 2 + 1) * HD * R + (int64_t)(wave * 16 + n) * R + 8 * g;
+    constexpr int EARLY = R / 64;  // (half of them: with all, two workgroups would not fit a compute unit's registers)
     bf16x8 wf[R / 32];
     if (wave < VT)
 #pragma unroll
-        for (int j = 0; j < R / 32; ++j) wf[j] = *(const bf16x8*)(w + 32 * j);
+        for (int j = 0; j < EARLY; ++j) wf[j] = *(const bf16x8*)(w + 32 * j);
     {
         constexpr int THREADS = 512 / SB, LANES = THREADS < 64 ? THREADS : 64;
         const int i = tid / THREADS, d0 = tid % THREADS * PER, s = s0 + i, chunk = d0 / (R / 8);
@@ -392,6 +394,8 @@ __global__ __launch_bounds__(512) void finish_kernel(const LatentShape sh, const
         a.lse[(int64_t)(s0 + tid) * H + h] = (norm[tid] + dot * sh.scale_log2e) * 0.6931471805599453f;
     }
     if (wave >= VT) return;
+#pragma unroll
+    for (int j = EARLY; j < R / 32; ++j) wf[j] = *(const bf16x8*)(w + 32 * j);
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < R / 32; ++j) {
