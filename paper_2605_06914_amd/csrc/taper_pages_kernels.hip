@@ -32,12 +32,25 @@ __global__ __launch_bounds__(256) void pages_copy_few_kernel(const PoolPointers 
     copy_piece(pools, args.move[blockIdx.x], blockIdx.z, page_bytes, blockIdx.y);
 }
 
-// One destination page (of one layer and tile group) a workgroup.  16 lanes find where the page's tokens come from; K and latent
-// tiles ([d / 8][16][8]) are then 16-byte pieces, V tiles ([16 / 4][d][4]) four tokens of a d.
+// Joins.  A workgroup has one destination page of one layer, or some heads of it.  16 lanes find where the page's tokens come from; K and
+// latent tiles ([d / 8][16][8]) are then 16-byte pieces.  V tiles ([16 / 4][d][4]) hold 4 tokens of a d in 8 bytes: where a group of 4
+// comes from consecutive tokens, also across a page's end, it is shifted out of the two groups it lies in (a token at a time, 2 bytes
+// each, took 263 us for 0.46 GB moved); where a run of tokens ends in between, it is gathered.
+struct Quarter {
+    long long first, second;  // byte offsets of the two groups (in a tile of head 0)
+    int shift;                // bits of the first that are not wanted, -1: gather, -2: no token
+};
+template <int KIND, int D>
 __global__ __launch_bounds__(256) void pages_pack_kernel(const PoolPointers pools, const PackArgs a) {
+    constexpr bool KV = KIND == TAPER_PAGES_KV;
+    constexpr int TILE = D * 32, UN = 4;
     __shared__ int src_page[16], src_tok[16];
+    __shared__ long long src_at[16];  // of a token in a K tile: its page and its place in a group of 8 dims
+    __shared__ Quarter quarter[4];
     const PackPage pg = a.pages[blockIdx.x];
     const int t = threadIdx.x;
+    const int heads = KV ? a.n_heads : 1;
+    const long long page_bytes = (long long)TILE * heads * (KV ? 2 : 1);
     if (t < 16) {
         int page = -1, tok = 0;
         if (t < pg.n_tokens) {
@@ -54,34 +67,70 @@ __global__ __launch_bounds__(256) void pages_pack_kernel(const PoolPointers pool
         }
         src_page[t] = page;
         src_tok[t] = tok;
+        src_at[t] = page < 0 ? -1 : page * page_bytes + tok * 16;
+    }
+    __syncthreads();
+    if (KV && t < 4) {
+        const int p0 = src_page[4 * t], p3 = src_page[4 * t + 3], t0 = src_tok[4 * t];
+        bool in_row = p3 >= 0;
+        for (int j = 1; j < 4; ++j) in_row = in_row && src_tok[4 * t + j] == ((t0 + j) & 15) && src_page[4 * t + j] == (t0 + j < 16 ? p0 : p3);
+        const int q0 = t0 >> 2;
+        Quarter q;
+        q.shift = p0 < 0 ? -2 : (in_row ? (t0 & 3) * 16 : -1);
+        q.first = p0 * page_bytes + q0 * (D * 8);
+        q.second = (t0 & 3) == 0 ? q.first : (q0 < 3 ? p0 * page_bytes + (q0 + 1) * (D * 8) : p3 * page_bytes);
+        quarter[t] = q;
     }
     __syncthreads();
     char* pool = (char*)pools.base[blockIdx.z];
-    const int D = a.dim, per_k = D * 2;  // 16-byte pieces of a K tile
-    const int64_t tile = (int64_t)D * 32, page_bytes = tile * a.n_heads * (a.kind == TAPER_PAGES_KV ? 2 : 1);
-    for (int i = blockIdx.y * 256 + t; i < a.n_heads * per_k; i += gridDim.y * 256) {
-        const int head = i / per_k, d8 = i % per_k >> 4, tok = i & 15;
-        if (src_page[tok] < 0) continue;
-        const int64_t at = head * tile + d8 * 256;
-        *(u32x4*)(pool + pg.dst * page_bytes + at + tok * 16) = *(const u32x4*)(pool + src_page[tok] * page_bytes + at + src_tok[tok] * 16);
+    char* const to = pool + pg.dst * page_bytes;
+    const int step = gridDim.y * 256;
+    const int n_k = heads * (D * 2);  // 16-byte pieces of the K tiles
+    for (int i0 = blockIdx.y * 256 + t; i0 < n_k; i0 += UN * step) {
+        u32x4 v[UN];
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+            const int i = i0 + u * step, head = i / (D * 2), d8 = i % (D * 2) >> 4;
+            if (i < n_k && src_at[i & 15] >= 0) v[u] = *(const u32x4*)(pool + src_at[i & 15] + (long long)head * TILE + d8 * 256);
+        }
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+            const int i = i0 + u * step;
+            if (i < n_k && src_at[i & 15] >= 0) *(u32x4*)(to + (long long)i * 16) = v[u];
+        }
     }
-    if (a.kind != TAPER_PAGES_KV) return;
-    const int per_v = D * 4;  // groups of four tokens of a d
-    for (int i = blockIdx.y * 256 + t; i < a.n_heads * per_v; i += gridDim.y * 256) {
-        const int head = i / per_v, q = i % per_v / D, d = i % D;
-        const int64_t at = (a.n_heads + head) * tile + d * 8;
-        unsigned short* to = (unsigned short*)(pool + pg.dst * page_bytes + at + q * D * 8);
-        unsigned short v[4];
+    if (!KV) return;
+    pool += (long long)heads * TILE;  // (the V tiles)
+    char* const to_v = to + (long long)heads * TILE;
+    const int n_v = heads * (D * 4);  // groups of four tokens of a d
+    for (int i0 = blockIdx.y * 256 + t; i0 < n_v; i0 += UN * step) {
+        unsigned long long x[UN], y[UN];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (src_page[4 * q + j] >= 0)
-                v[j] = *(const unsigned short*)(pool + src_page[4 * q + j] * page_bytes + at + (src_tok[4 * q + j] >> 2) * (D * 8) + (src_tok[4 * q + j] & 3) * 2);
-        if (src_page[4 * q + 3] >= 0) {
-            *(u32x2*)to = u32x2{v[0] | (unsigned)v[1] << 16, v[2] | (unsigned)v[3] << 16};
-        } else {
+        for (int u = 0; u < UN; ++u) {
+            const int i = i0 + u * step, head = i / (D * 4), d = i % D;
+            if (i >= n_v) continue;
+            const Quarter& q = quarter[i / D % 4];
+            const long long at = (long long)head * TILE + d * 8;
+            if (q.shift >= 0) {
+                x[u] = *(const unsigned long long*)(pool + q.first + at);
+                y[u] = *(const unsigned long long*)(pool + q.second + at);
+            }
+        }
 #pragma unroll
-            for (int j = 0; j < 3; ++j)
-                if (src_page[4 * q + j] >= 0) to[j] = v[j];
+        for (int u = 0; u < UN; ++u) {
+            const int i = i0 + u * step, head = i / (D * 4), d = i % D, qi = i / D % 4;
+            if (i >= n_v) continue;
+            const int shift = quarter[qi].shift;
+            if (shift >= 0) {
+                *(unsigned long long*)(to_v + (long long)i * 8) = shift ? x[u] >> shift | y[u] << (64 - shift) : x[u];
+            } else if (shift == -1) {
+                for (int j = 0; j < 4; ++j) {
+                    const int k = 4 * qi + j;
+                    if (src_page[k] < 0) break;
+                    const char* from = pool + src_page[k] * page_bytes + (long long)head * TILE + (src_tok[k] >> 2) * (D * 8) + d * 8 + (src_tok[k] & 3) * 2;
+                    *(unsigned short*)(to_v + (long long)i * 8 + j * 2) = *(const unsigned short*)from;
+                }
+            }
         }
     }
 }
@@ -102,13 +151,22 @@ hipError_t launch_pages_copy(const PoolPointers& pools, int n_layers, const Page
     return hipGetLastError();
 }
 
-hipError_t launch_pages_pack(const PoolPointers& pools, int n_layers, const PackArgs& a, hipStream_t s) {
+template <int KIND, int D>
+static void launch_pack_as(const PoolPointers& pools, int n_layers, const PackArgs& a, hipStream_t s) {
     const int split = a.n_heads >= 4 ? 2 : 1;
     for (int64_t i = 0; i < a.n_pages; i += kMostBlocks) {
         PackArgs b = a;
         b.pages += i;
-        hipLaunchKernelGGL(pages_pack_kernel, dim3((unsigned)(a.n_pages - i < kMostBlocks ? a.n_pages - i : kMostBlocks), split, n_layers), dim3(256), 0, s, pools, b);
+        hipLaunchKernelGGL((pages_pack_kernel<KIND, D>), dim3((unsigned)(a.n_pages - i < kMostBlocks ? a.n_pages - i : kMostBlocks), split, n_layers), dim3(256), 0, s, pools, b);
     }
+}
+
+hipError_t launch_pages_pack(const PoolPointers& pools, int n_layers, const PackArgs& a, hipStream_t s) {
+    if (a.kind == TAPER_PAGES_KV && a.dim == 128) launch_pack_as<TAPER_PAGES_KV, 128>(pools, n_layers, a, s);
+    else if (a.kind == TAPER_PAGES_KV && a.dim == 64) launch_pack_as<TAPER_PAGES_KV, 64>(pools, n_layers, a, s);
+    else if (a.kind == TAPER_PAGES_LATENT && a.dim == 576) launch_pack_as<TAPER_PAGES_LATENT, 576>(pools, n_layers, a, s);
+    else if (a.kind == TAPER_PAGES_LATENT && a.dim == 320) launch_pack_as<TAPER_PAGES_LATENT, 320>(pools, n_layers, a, s);
+    else return hipErrorInvalidValue;
     return hipGetLastError();
 }
 

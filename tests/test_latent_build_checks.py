@@ -10,7 +10,7 @@ import pytest
 from paper_2605_06914_amd.build import CSRC, HIP_FLAGS, ROOT
 from tests.asm_hazards import scan, scan_scalar_addresses
 
-SOURCES = {"taper_latent_kernels.hip": 13, "taper_prompt_kernels.hip": 8, "taper_pages_kernels.hip": 3}
+SOURCES = {"taper_latent_kernels.hip": 13, "taper_prompt_kernels.hip": 8, "taper_pages_kernels.hip": 6}
 
 
 @pytest.fixture(scope="module", params=SOURCES, ids=lambda s: s.split(".")[0])
