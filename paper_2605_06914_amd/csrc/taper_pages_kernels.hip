@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256) void pages_copy_few_kernel(const PoolPointers 
 // Joins.  A workgroup has one destination page of one layer, or some heads of it.  16 lanes find where the page's tokens come from; K and
 // latent tiles ([d / 8][16][8]) are then 16-byte pieces.  V tiles ([16 / 4][d][4]) hold 4 tokens of a d in 8 bytes: where a group of 4
 // comes from consecutive tokens, also across a page's end, it is shifted out of the two groups it lies in (a token at a time, 2 bytes
-// each, took 263 us for 0.46 GB moved); where a run of tokens ends in between, it is gathered.
+// each, took 263 us for 0.46 GB moved, this 204); where a run of tokens ends in between, it is gathered.
 struct Quarter {
     long long first, second;  // byte offsets of the two groups (in a tile of head 0)
     int shift;                // bits of the first that are not wanted, -1: gather, -2: no token
@@ -43,7 +43,7 @@ struct Quarter {
 template <int KIND, int D>
 __global__ __launch_bounds__(256) void pages_pack_kernel(const PoolPointers pools, const PackArgs a) {
     constexpr bool KV = KIND == TAPER_PAGES_KV;
-    constexpr int TILE = D * 32, UN = 4;
+    constexpr int TILE = D * 32, UN = 8;
     __shared__ int src_page[16], src_tok[16];
     __shared__ long long src_at[16];  // of a token in a K tile: its page and its place in a group of 8 dims
     __shared__ Quarter quarter[4];
@@ -91,12 +91,12 @@ __global__ __launch_bounds__(256) void pages_pack_kernel(const PoolPointers pool
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
             const int i = i0 + u * step, head = i / (D * 2), d8 = i % (D * 2) >> 4;
-            if (i < n_k && src_at[i & 15] >= 0) v[u] = *(const u32x4*)(pool + src_at[i & 15] + (long long)head * TILE + d8 * 256);
+            if (i < n_k && src_at[i & 15] >= 0) v[u] = __builtin_nontemporal_load((const u32x4*)(pool + src_at[i & 15] + (long long)head * TILE + d8 * 256));
         }
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
             const int i = i0 + u * step;
-            if (i < n_k && src_at[i & 15] >= 0) *(u32x4*)(to + (long long)i * 16) = v[u];
+            if (i < n_k && src_at[i & 15] >= 0) __builtin_nontemporal_store(v[u], (u32x4*)(to + (long long)i * 16));
         }
     }
     if (!KV) return;
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256) void pages_pack_kernel(const PoolPointers pool
             if (i >= n_v) continue;
             const int shift = quarter[qi].shift;
             if (shift >= 0) {
-                *(unsigned long long*)(to_v + (long long)i * 8) = shift ? x[u] >> shift | y[u] << (64 - shift) : x[u];
+                __builtin_nontemporal_store(shift ? x[u] >> shift | y[u] << (64 - shift) : x[u], (unsigned long long*)(to_v + (long long)i * 8));
             } else if (shift == -1) {
                 for (int j = 0; j < 4; ++j) {
                     const int k = 4 * qi + j;
@@ -153,7 +153,7 @@ hipError_t launch_pages_copy(const PoolPointers& pools, int n_layers, const Page
 
 template <int KIND, int D>
 static void launch_pack_as(const PoolPointers& pools, int n_layers, const PackArgs& a, hipStream_t s) {
-    const int split = a.n_heads >= 4 ? 2 : 1;
+    const int split = a.n_heads >= 4 && (int64_t)a.n_pages * n_layers < 1024 ? 4 : 1;  // (finding the tokens is done once a workgroup)
     for (int64_t i = 0; i < a.n_pages; i += kMostBlocks) {
         PackArgs b = a;
         b.pages += i;
