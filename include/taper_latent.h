@@ -50,7 +50,7 @@ typedef struct taper_latent_ctx taper_latent_ctx;
 typedef struct taper_latent_plan taper_latent_plan;
 
 TAPER_LATENT_API int taper_latent_create(const taper_latent_config *cfg /* host */, taper_latent_ctx **out_ctx);
-TAPER_LATENT_API void taper_latent_destroy(taper_latent_ctx *ctx);
+TAPER_LATENT_API void taper_latent_destroy(taper_latent_ctx *ctx); /* synchronises the device: not while a stream is being recorded */
 
 /* One unit of a decode step's work: n_tokens tokens from block-table entry page0 of row seq0 on, against n_rows query rows
  * (row = sequence * n_heads + head) from row0 on; its partial rows start at part_row.  n_rows 0: nothing (filler). */
@@ -72,7 +72,8 @@ typedef struct {
  * checks and their statuses (seg_start may be NULL: one private segment per sequence).  One plan serves every layer
  * of the step.  A plan owns the partial rows and rewritten queries of its calls, so two plans never share a
  * workspace; the calls of one plan must be ordered on one stream, or by events.  target_workgroups 0: as many as the
- * device has compute units (256 on a host-only context).  Memory of a freed plan is used again by later plans of the
+ * device has compute units (256 on a host-only context).  TAPER_EINVAL on a stream that is being recorded into a graph.
+ * Memory of a freed plan is used again by later plans of the
  * context, whose calls must be ordered behind its own.  Not safe to call concurrently on one ctx.  Plans are freed
  * before their context is destroyed.
  */

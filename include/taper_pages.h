@@ -72,7 +72,7 @@ typedef struct {
 typedef struct taper_mover taper_mover; /* holds the lists of calls in flight */
 
 TAPER_PAGES_API int taper_mover_create(const taper_page_format *format /* host */, taper_mover **out_mover);
-TAPER_PAGES_API void taper_mover_destroy(taper_mover *mover); /* synchronises the device */
+TAPER_PAGES_API void taper_mover_destroy(taper_mover *mover); /* synchronises the device: not while a stream is being recorded */
 /*
  * Page dst[i] becomes a copy of page src[i], in each of the n_layers pools (one launch for all of them; each of
  * n_pool_pages pages, 16-byte aligned).  A source may be copied several times.  TAPER_EBLOCK for a page outside the pool,

@@ -44,6 +44,13 @@ class OnDevice {
     bool changed_ = false;
 };
 
+// Whether what is enqueued on `s` is recorded into a graph.
+inline bool recording(hipStream_t s) {
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(s, &status) != hipSuccess) (void)hipGetLastError();  // (the launch itself will say what is wrong)
+    return status != hipStreamCaptureStatusNone;
+}
+
 // No C++ exception leaves a C entry point.
 template <typename F>
 int guarded(F&& f) {

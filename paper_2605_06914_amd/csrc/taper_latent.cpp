@@ -127,6 +127,7 @@ class Layout {
 };
 
 int upload(taper_latent_plan* plan, const Layout& lay, size_t image, hipStream_t s) {
+    if (taper::recording(s)) return set_error(TAPER_EINVAL, "a plan cannot be built on a stream that is being recorded");
     const int st = acquire(plan->ctx, image, lay.total(), &plan->buf);
     if (st != TAPER_OK) return st;
     lay.write(plan->buf.staging);

@@ -17,6 +17,7 @@ using taper::aligned;
 using taper::guarded;
 using taper::hip_error;
 using taper::OnDevice;
+using taper::recording;
 using taper::set_error;
 
 struct taper_page_pool {
@@ -100,12 +101,6 @@ int next_lists(taper_mover* m, size_t bytes, MoveLists** out) {
     }
     *out = &l;
     return TAPER_OK;
-}
-
-bool recording(hipStream_t s) {
-    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-    if (hipStreamIsCapturing(s, &status) != hipSuccess) (void)hipGetLastError();
-    return status != hipStreamCaptureStatusNone;
 }
 
 template <typename Launch>

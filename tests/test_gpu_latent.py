@@ -1,10 +1,19 @@
 """Latent-cache attention (decode step and prompts) and append on the GPU against the definition in 64 bits."""
+import gc
+
 import numpy as np
 import pytest
 
 from tests.latent_ref import RMS, ROPE, Batch, attention, pool_of, rows_of, to_bf16, values
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _nothing_left_to_collect():
+    """Objects of the test before that only the collector frees: their end waits for the device, which no stream that is being
+    recorded survives."""
+    gc.collect()
 
 
 def dev(x, dtype=None):
@@ -385,3 +394,74 @@ def test_a_request_from_its_prompt_through_branches_and_their_join():
         out = torch.empty(1, H, hd, dtype=torch.bfloat16, device="cuda:0")
         ctx.decode_step_attention(plan, dev(q), w_d, pools[l], out)
         compare(q, out.double().cpu().numpy(), [np.concatenate([prompt[l, :80], *[np.stack([t[l] for t in own[i]]) for i in range(2)]])])
+
+
+def test_a_plan_is_not_built_on_a_stream_that_is_being_recorded():
+    import torch
+    from paper_2605_06914_amd import TAPER_EINVAL, TaperError
+    ctx, d = context(16, 512, 128), setup(9)
+    plan = plan_of(ctx, d["b"])
+    side, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        ctx.decode_step_attention(plan, d["q"], d["w"], d["pages"], d["out"])
+        for prompt in (False, True):
+            with pytest.raises(TaperError) as e:
+                plan_of(ctx, d["b"], prompt)
+            assert e.value.status == TAPER_EINVAL
+    g.replay()
+    torch.cuda.synchronize()
+    assert d["out"].float().abs().sum() > 0
+
+
+def test_pages_beyond_four_gigabytes():
+    """The far end of a pool of 4.6 GB: append, copy, decode step and prompt there."""
+    import torch
+    from paper_2605_06914_amd import PageMover
+    H, R, hd, n_pages = 8, 512, 128, 250000
+    pages = torch.zeros(n_pages, 72, 16, 8, dtype=torch.bfloat16, device="cuda:0")
+    rng = np.random.default_rng(3)
+    b = Batch([(0, [[100]]), (40, [[9], [33]])], 50, new=[7, 9, 3])
+    q, w, tok = values(b, H, R, hd, 51)
+    far = n_pages - 1 - rng.permutation(60)[:b.n_pages].astype(np.int64)  # where each page of the batch lies
+    live = np.nonzero(np.isfinite(tok[:, 0]))[0]
+    ctx, mover = context(H, R, hd), PageMover.latent(R, device=0)
+    rows = dev(tok[live])
+    ctx.append(rows[:, :R], rows[:, R:], dev((far[live // 16] - 100) * 16 + live % 16), pages, n_pages)
+    mover.copy([pages], far - 100, far, n_pages)
+    b.table = np.where(b.table >= 0, far[b.table], -1).astype(np.int32)
+    b.n_pages = n_pages
+    plan = ctx.prompt_plan_build(b.table, b.group, b.prefix, b.seg_len, b.new, n_pages)
+    out = torch.empty(19, H, hd, dtype=torch.bfloat16, device="cuda:0")
+    ctx.prompt_attention(plan, dev(q), dev(w), pages, out)
+    back = np.full_like(tok, np.nan)
+    back[live] = tok[live]
+    near = Batch([(0, [[100]]), (40, [[9], [33]])], 50, new=[7, 9, 3])
+    want = attention(near, q, w, back, H, R, hd, (hd + ROPE) ** -0.5, False)
+    assert (np.abs(out.double().cpu().numpy() - want[0]) <= want[2]).all()
+    plan = ctx.plan_build(b.table, b.group, b.prefix, b.seg_len, n_pages)
+    ctx.decode_step_attention(plan, dev(q[:3]), dev(w), pages, out)
+    near.new[:] = 1
+    want = attention(near, q[:3], w, back, H, R, hd, (hd + ROPE) ** -0.5, True)
+    assert (np.abs(out[:3].double().cpu().numpy() - want[0]) <= want[2]).all()
+
+
+def test_heads_whose_keys_and_values_are_expanded_in_turns():
+    """256 heads of 36000 tokens are 4.7 GB: more than are expanded at a time.  Some heads of both turns."""
+    import torch
+    H, R, hd, T, n = 256, 512, 128, 36000, 5
+    b = Batch([(0, [[T]])], 60, new=[n])
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(1)
+    make = lambda *shape, std=1.0: torch.empty(shape, dtype=torch.bfloat16, device="cuda:0").normal_(0.0, std, generator=gen)
+    q, w, pages = make(n, H, hd + ROPE), make(H, 2 * hd, R, std=R ** -0.5), make(b.n_pages, 72, 16, 8)
+    ctx = context(H, R, hd)
+    plan = plan_of(ctx, b, True)
+    out, lse = torch.empty(n, H, hd, dtype=torch.bfloat16, device="cuda:0"), torch.empty(n, H, device="cuda:0")
+    ctx.prompt_attention(plan, q, w, pages, out, lse)
+    torch.cuda.synchronize()
+    plan.free()
+    some = [0, 100, 231, 232, 233, 255]
+    tok = rows_of(pages.float().cpu().numpy())
+    want = attention(b, q.float().cpu().numpy()[:, some], w.float().cpu().numpy()[some], tok, len(some), R, hd, (hd + ROPE) ** -0.5, False)
+    assert (np.abs(out.double().cpu().numpy()[:, some] - want[0]) <= want[2]).all()
+    assert (np.abs(lse.double().cpu().numpy()[:, some] - want[1]) <= want[3]).all()

@@ -1,10 +1,19 @@
 """Page copies and joins on the GPU against indexing on the CPU, bit for bit."""
+import gc
+
 import numpy as np
 import pytest
 
 from tests.latent_ref import Batch, pages_of, pool_of, rows_of
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _nothing_left_to_collect():
+    """Objects of the test before that only the collector frees: their end waits for the device, which no stream that is being
+    recorded survives."""
+    gc.collect()
 FORMATS = [("kv", 8, 128), ("kv", 1, 64), ("kv", 3, 128), ("latent", 1, 576), ("latent", 1, 320)]
 
 
