@@ -8,7 +8,7 @@
 //
 // Expanded keys and values are half precision, and so are the weights they meet: 11 bits of each instead of bf16's 8.  Four pages
 // whose keys (or values) half precision does not hold, beyond 65504 or all of them below 2^-10, are bf16 instead; `format` says
-// which.  A query's part without rotation is brought into half precision's range by a power of two of its own, exactly.
+// which.  A query's part without rotation is brought into half precision's range by a power of two of its own.
 #include <cmath>
 #include <type_traits>
 
@@ -175,6 +175,10 @@ __global__ __launch_bounds__(512, 2) void expand_kernel(const PromptArgs a, cons
 // the layout that O^T = V^T P^T takes them in.
 // ---------------------------------------------------------------------------
 constexpr int kStages = 3;
+// Weights are made 2^10 times as large: half precision ends at 2^-24, and tokens whose weights are that far below the largest may still
+// be so many that they matter (64000 of weight 2^-24 are a 256th).  At 2^10 those of 2^-34 are kept, and 2^6 is left to its upper end
+// for the rounding of large scores.
+constexpr float kWeightBits = 10.f;
 template <int HD>
 struct PromptSmem {
     _Float16 k[kStages][4][HD * 16];
@@ -248,14 +252,23 @@ __global__ __launch_bounds__(512, 2) void prompt_kernel(const LatentShape sh, co
 #pragma unroll
             for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(v[j][i]));
         }
-        const int e = exponent_of(max_lane_groups(most));
+        // q_n in [0.5, 1), but q_r at most 2^20 (its products with r shall not overflow where q_n is all but nothing; q_n's last bit is
+        // then below 2^-44 of the query), and c a normal number
+        bf16x8 rot[2];
+        float most_r = 0.f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            rot[j] = *(const bf16x8*)(q + HD + 32 * j);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most_r = fmaxf(most_r, fabsf((float)rot[j][i]));
+        }
+        const int e = max(max(exponent_of(max_lane_groups(most)), exponent_of(max_lane_groups(most_r)) - 20), -100);
         const float down = __uint_as_float((unsigned)(127 - e) << 23);
         c[k] = sh.scale_log2e * __uint_as_float((unsigned)(127 + e) << 23);
 #pragma unroll
         for (int j = 0; j < KS; ++j) qf[k][j] = __builtin_convertvector(v[j] * down, f16x8);
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-            qr[k][j] = __builtin_convertvector(__builtin_convertvector(*(const bf16x8*)(q + HD + 32 * j), f32x8) * down, bf16x8);
+        for (int j = 0; j < 2; ++j) qr[k][j] = __builtin_convertvector(__builtin_convertvector(rot[j], f32x8) * down, bf16x8);
     }
     const int first_pos = t.first_pos + min(32 * wave, t.n_rows - 1), last_pos = t.first_pos + min(32 * wave + 31, t.n_rows - 1);  // of this wave's rows
     const bool idle = 32 * wave >= t.n_rows, few = a.lse && first_pos < kLowPositions;
@@ -366,14 +379,14 @@ __global__ __launch_bounds__(512, 2) void prompt_kernel(const LatentShape sh, co
                 for (int d = 0; d < DT; ++d) O[k][d] *= alpha;
                 m[k] = mn;
             }
-            const float ref = m[k] == -INFINITY ? 0.f : m[k];  // (a row may see nothing of these pages)
+            const float ref = m[k] == -INFINITY ? 0.f : m[k] - kWeightBits;  // (a row may see nothing of these pages)
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
                 f32x4 w;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w[i] = fast_exp2(fmaf(s[p][k][i], c[k], -ref));
                 l[k] += (w[0] + w[1]) + (w[2] + w[3]);
-                // (weights of at most 1, in the type of the values they meet)
+                // (in the type of the values they meet)
                 pr[p][k] = PLAIN || !format[(p & 2) + 1] ? __builtin_bit_cast(uint2, __builtin_convertvector(w, f16x4)) : __builtin_bit_cast(uint2, __builtin_convertvector(w, bf16x4));
             }
         }
@@ -411,12 +424,12 @@ __global__ __launch_bounds__(512, 2) void prompt_kernel(const LatentShape sh, co
         const float inv = total > 0.f ? 1.0f / total : total;  // (NaN stays what it is)
         if (t.part_row >= 0) {
             const int64_t at = (int64_t)hl * a.n_partial_rows + t.part_row + r;
-            if (g == 0) a.ml[at] = make_float2(m[k], total);
+            if (g == 0) a.ml[at] = make_float2(m[k] - kWeightBits, total);
 #pragma unroll
             for (int d = 0; d < DT; ++d) *(f32x4*)(a.part + at * HD + 16 * d + 4 * g) = O[k][d] * inv;
         } else {
             const int64_t at = (int64_t)(t.row0 + r) * H + h;
-            if (g == 0 && a.lse) a.lse[at] = (m[k] + log2f(total)) * 0.6931471805599453f;
+            if (g == 0 && a.lse) a.lse[at] = (m[k] - kWeightBits + log2f(total)) * 0.6931471805599453f;
 #pragma unroll
             for (int d = 0; d < DT; ++d) *(bf16x4*)((__bf16*)a.out + at * HD + 16 * d + 4 * g) = __builtin_convertvector(O[k][d] * inv, bf16x4);
         }
