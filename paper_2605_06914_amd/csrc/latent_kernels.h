@@ -35,7 +35,7 @@ struct LatentDecodeArgs {
     const void* pages;
     void* out;
     float* lse;
-    int32_t bt_stride, n_seqs, n_items, row_tiles;  // row_tiles: the widest item's, in 16 rows
+    int32_t bt_stride, n_seqs, n_items;
 };
 hipError_t launch_latent_decode(const LatentShape& sh, const LatentDecodeArgs& a, hipStream_t s);
 

@@ -277,8 +277,9 @@ int build_decode(taper_latent_ctx* ctx, int n_seqs, const int32_t* block_table, 
     }
     const int st = taper::resolve_batch(cfg.page_size, n_seqs, block_table, stride, group, prefix, seg_start, seg_len, n_pool_pages, &plan->batch);
     if (st != TAPER_OK) return st;
-    if ((int64_t)n_seqs * cfg.n_heads > INT32_MAX / 2) return set_error(TAPER_EINVAL, "too many query rows");
-    make_decode_items(cfg, target_workgroups > 0 ? target_workgroups : ctx->units, plan);
+    // (32 threads a row, 16 sequences a workgroup of the grid's second axis: a launch takes less than 2^32 and 2^16)
+    if ((int64_t)n_seqs * cfg.n_heads > (1 << 26) || n_seqs > 16 * 65535) return set_error(TAPER_EINVAL, "too many query rows");
+    make_decode_items(cfg, target_workgroups > 0 ? std::min(target_workgroups, 1 << 16) : ctx->units, plan);
     if (plan->n_partial_rows > INT32_MAX || plan->items.size() > kMostBlocks) return set_error(TAPER_EINVAL, "too many query rows");
     const int KD = cfg.latent_dim + cfg.rope_dim;
     Layout lay;

@@ -2,7 +2,7 @@
 // a token, read once for all heads.
 //
 // Three launches.  absorb_kernel rewrites the queries, q_lat = (W_k[h]^T q_n, q_r).  latent_decode_kernel computes
-// softmax(scale q_lat . (c, r)) . c for items of up to 64 query rows and some tokens, as partial rows.  finish_kernel merges
+// softmax(scale q_lat . (c, r)) . c for items of up to 128 query rows and some tokens, as partial rows.  finish_kernel merges
 // a row's partials through their (max, sum) and applies W_v[h].
 #include <cmath>
 #include <type_traits>
@@ -75,16 +75,18 @@ __global__ __launch_bounds__(64) void absorb_kernel(const LatentShape sh, const 
 }
 
 // ---------------------------------------------------------------------------
-// The attention.  A workgroup of 4 waves, one on each SIMD, holds up to 128 query rows, 32 a wave, and takes 64 tokens (4 pages) at a
-// time through LDS.  A wave makes the scores of its rows, S^T = C Q^T, weighs them and adds the values, O^T = C^T P^T, by itself: its
-// queries (32 rows x 576 values: 144 registers) and accumulators (32 rows x 512 values: 256, the accumulation registers) stay with it,
-// the weights leave the score product in the layout that the value product takes them in, and waves meet once a tile.  K and V are
-// the same bytes; each wave reads them from LDS twice, 68 KiB for 272 products, which at 128 bytes a clock and 4 waves is as long as
-// the products take: what bounds a compute unit whose rows are many.  V's operand is columns of a token-major page:
-// ds_read_b64_tr_b16 reads 4 tokens x 16 columns transposed.
-// Bringing a tile to LDS blocks the waves that ask for it (1200 clocks for its 72 KiB from the L2, 2200 from memory), so many rows a
+// The attention.  A workgroup of 8 waves, two on each SIMD, holds up to 128 query rows, 16 a wave, and takes 64 tokens (4 pages, 72 KiB)
+// at a time through LDS.  A wave makes the scores of its rows, S^T = C Q^T, weighs them and adds the values, O^T = C^T P^T, by itself: its
+// queries (16 rows x 576 values: 72 registers) and accumulators (16 rows x 512 values: 128) stay with it, the weights leave the score
+// product in the layout that the value product takes them in, and waves meet once a tile.  K and V are the same bytes; V's operand is
+// columns of a token-major page: ds_read_b64_tr_b16 reads 4 tokens x 16 columns transposed.
+// What bounds it: every wave reads the whole tile from LDS, for K and for V, 1088 KiB a tile and workgroup, which at 128 bytes a clock
+// is 8700 clocks against 4350 of products.  (32 rows a wave, 4 waves, would halve that, but 144 + 256 registers leave none for operands
+// in flight: it spilled.  Two groups of 4 waves in turns, one at its products while the other weighs, took 884 us where this takes 793.)
+// Bringing a tile to LDS blocks the waves that ask for it (1230 clocks for its 72 KiB from the L2, 2200 from memory), so many rows a
 // tile matter (a workgroup of 64 rows, whose waves shared the work by pages and columns, took 6300 clocks a tile), and waves without
-// rows bring the tiles of items that have fewer than 97.
+// rows bring the tiles of items that leave some.  At 8 requests x 16 branches over 32768 shared tokens each and 32 single sequences, 64
+// heads: 696 us, 900 TF/s; 32 single sequences of 1024 to 4096 tokens at 16 heads: 38.5 us, of which the cache's bytes take 16.
 // ---------------------------------------------------------------------------
 // Weights are taken relative to a row's reference, the largest score of some earlier tile, so that a tile's weights do not wait for its
 // maximum.  A score that is more than this above its reference (in log2; a first tile always is) makes the wave take new references.

@@ -144,3 +144,12 @@ def test_calls_without_a_device_or_with_another_plan_are_refused():
     assert append(ctx._h, 4, any_ptr, 511, any_ptr, 64, any_ptr, any_ptr, 10, None) == TAPER_EINVAL
     assert append(ctx._h, 4, any_ptr, 520, any_ptr, 60, any_ptr, any_ptr, 10, None) == TAPER_EINVAL
     assert append(ctx._h, 4, any_ptr, 512, any_ptr, 64, any_ptr, any_ptr, 0, None) == TAPER_EINVAL
+
+
+def test_as_many_workgroups_as_an_integer_holds_and_more_rows_than_a_launch():
+    b = Batch([(0, [[5000]]), (100, [[0], [17], [300]])], 2)
+    e = host().plan_build(b.table, b.group, b.prefix, b.seg_len, b.n_pages, target_workgroups=2 ** 31 - 1, seg_start=b.seg_start).export()
+    assert sum(r * n for _, _, n, _, r, _ in e["items"].tolist()) == 16 * (5000 + 3 * 100 + 317)
+    for H, n in ((1, 16 * 65535 + 1), (256, 2 ** 18 + 1)):
+        ones = np.ones(n, np.int32)
+        refused(TAPER_EINVAL, host(H).plan_build, np.arange(n, dtype=np.int32)[:, None], np.arange(n, dtype=np.int32), 0 * ones, ones, n)
