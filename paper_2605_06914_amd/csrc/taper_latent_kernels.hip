@@ -81,12 +81,13 @@ __global__ __launch_bounds__(64) void absorb_kernel(const LatentShape sh, const 
 // product in the layout that the value product takes them in, and waves meet once a tile.  K and V are the same bytes; V's operand is
 // columns of a token-major page: ds_read_b64_tr_b16 reads 4 tokens x 16 columns transposed.
 // What bounds it: every wave reads the whole tile from LDS, for K and for V, 1088 KiB a tile and workgroup, which at 128 bytes a clock
-// is 8700 clocks against 4350 of products.  (32 rows a wave, 4 waves, would halve that, but 144 + 256 registers leave none for operands
+// is 8700 clocks against 4350 of products (the counters: LDS active for 0.38, matrix units for 0.40 of the time; the rest is waits of two
+// waves a SIMD for operands, the tile's meeting and the issue of the next one).  (32 rows a wave, 4 waves, would halve that, but 144 + 256 registers leave none for operands
 // in flight: it spilled.  Two groups of 4 waves in turns, one at its products while the other weighs, took 884 us where this takes 793.)
 // Bringing a tile to LDS blocks the waves that ask for it (1230 clocks for its 72 KiB from the L2, 2200 from memory), so many rows a
 // tile matter (a workgroup of 64 rows, whose waves shared the work by pages and columns, took 6300 clocks a tile), and waves without
 // rows bring the tiles of items that leave some.  At 8 requests x 16 branches over 32768 shared tokens each and 32 single sequences, 64
-// heads: 696 us, 900 TF/s; 32 single sequences of 1024 to 4096 tokens at 16 heads: 38.5 us, of which the cache's bytes take 16.
+// heads: 660 us, 950 TF/s; 32 single sequences of 1024 to 4096 tokens at 16 heads: 38.5 us, of which the cache's bytes take 16.
 // ---------------------------------------------------------------------------
 // Weights are taken relative to a row's reference, the largest score of some earlier tile, so that a tile's weights do not wait for its
 // maximum.  A score that is more than this above its reference (in log2; a first tile always is) makes the wave take new references.
@@ -111,7 +112,12 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
 
     auto page = [&](int t, int pg) { return pages + (int64_t)row[min(4 * t + pg, last_page)] * (PAGE * 2); };  // (past the end: the last one)
     auto place = [&](int t, int pg) { return uniform(lds_address(sm.tile[t & 1][pg])); };
-    auto load = [&](const char* from, unsigned to, int i) { load_to_lds(from + i * 1024, lane * 16, to + i * 1024); };  // (scalar sums: one lane offset for all)
+    // In LDS every other row of 16 tokens has its fours of tokens in the opposite order: V's operand takes 8 tokens of two rows at a time,
+    // which would lie in the same banks (a third of the LDS's time went by in such conflicts), and K's 16-byte reads, which meet eight tokens
+    // of each of two rows as well, stay without any.  (Not where waves only bring tiles: that takes 2 % longer so, and conflicts do not matter.)
+    constexpr int TURN = FULL ? 12 : 0;
+    const int lane_from = (lane ^ (lane >> 4 & 1) * TURN) * 16;
+    auto load = [&](const char* from, unsigned to, int i) { load_to_lds(from + i * 1024, lane_from, to + i * 1024); };  // (scalar sums: one lane offset for all)
     constexpr int LOADS = PAGE / 1024;  // of half a page
     if (!FULL && wave >= busy) {  // bring the tiles
         const int others = 8 - busy;
@@ -176,14 +182,14 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
                 const int valid = it.n_tokens - 64 * t - 16 * pg;
                 if (valid >= 16) continue;
                 for (int i = lane; i < KD / 8 * 16; i += 64)
-                    if ((i & 15) >= valid) *(u32x4*)(sm.tile[t & 1][pg] + i * 8) = u32x4{0, 0, 0, 0};
+                    if (((i ^ (i >> 4 & 1) * TURN) & 15) >= valid) *(u32x4*)(sm.tile[t & 1][pg] + i * 8) = u32x4{0, 0, 0, 0};
             }
         }
         f32x4 s[4][NT];
         constexpr int AHEAD = 2;  // steps of two pages' operands in flight
 #pragma unroll
         for (int half = 0; half < 2; ++half) {  // two pages at a time: twice as many chains of products
-            const __bf16* const k_at = tile + half * 2 * PAGE + g * 128 + n * 8;
+            const __bf16* const k_at = tile + half * 2 * PAGE + lane_from / 2;
             bf16x8 kf[AHEAD][2];
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j)
@@ -239,7 +245,7 @@ DEV void decode_item(const LatentShape& sh, const LatentDecodeArgs& a, const tap
                 l[k] += (w[0] + w[1]) + (w[2] + w[3]);
                 pr[p][k] = __builtin_convertvector(w, bf16x4);  // (8 bits of each weight)
             }
-        const __bf16* const v_at = tile + (lane >> 1 & 1) * 128 + (4 * g + (n >> 2)) * 8 + (lane & 1) * 4;
+        const __bf16* const v_at = tile + (lane >> 1 & 1) * 128 + ((4 * g + (n >> 2)) ^ (lane >> 1 & 1) * TURN) * 8 + (lane & 1) * 4;
         auto columns = [&](int x) {  // 16 columns of 32 tokens; x: column group, then pair of pages
             typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
             const __bf16* at = v_at + x / DT * 2 * PAGE + x % DT * 256;
