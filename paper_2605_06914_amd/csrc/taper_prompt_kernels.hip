@@ -28,7 +28,7 @@ DEV float max_wave(float v) {
 
 // ---------------------------------------------------------------------------
 // expand: a product of (tokens x R) and (R x 2 head_dim) for each head.  A workgroup keeps 128 rows of W in LDS (R = 512: 128 KiB,
-// read 1 KiB an operand, each 16-byte piece moved by its row so that 8 rows' pieces lie in different banks) and its 8 waves go through
+// read 1 KiB an operand, each 16-byte piece moved by its row so that 16 rows' pieces lie in different banks) and its 8 waves go through
 // the tokens 64 at a time, each by itself: a page's operands come straight from the cache, 1 KiB in a row each, and nothing but W is
 // shared, so no wave waits for another.  Keys come out as W C^T (a lane: 4 consecutive d of a token), values as C W^T (4 consecutive
 // tokens of a d).
@@ -47,11 +47,11 @@ DEV void expand_chunk(const PromptArgs& a, const __bf16* w, const int hl, const 
         page[i] = (const __bf16*)a.pages + (int64_t)uniform(a.e_page[e]) * (KD * 16);
         valid[i] = uniform(a.e_valid[e]);
     }
-    const __bf16* w_at[2][2];  // where this lane reads W for even and odd steps, its first and its last 64 rows
+    const __bf16* w_at[4][2];  // where this lane reads W in each of four steps, its first and its last 64 rows
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < 4; ++x)
 #pragma unroll
-        for (int y = 0; y < 2; ++y) w_at[x][y] = w + (64 * y + n) * R + ((4 * x + g) ^ (n & 7)) * 8;
+        for (int y = 0; y < 2; ++y) w_at[x][y] = w + (64 * y + n) * R + ((4 * x + g) ^ n) * 8;
     f32x4 acc[4][8];
     bf16x8 cf[AHEAD][4];
 #pragma unroll
@@ -71,7 +71,7 @@ DEV void expand_chunk(const PromptArgs& a, const __bf16* w, const int hl, const 
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const bf16x8 wf = *(const bf16x8*)(w_at[k & 1][j / 4] + (16 * (j % 4)) * R + (k >> 1) * 64);
+            const bf16x8 wf = *(const bf16x8*)(w_at[k & 3][j / 4] + (16 * (j % 4)) * R + (k >> 2) * 128);
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[i][j] = is_value(j) ? mfma16(c[i], wf, acc[i][j]) : mfma16(wf, c[i], acc[i][j]);
         }
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(512, 2) void expand_kernel(const PromptArgs a, cons
 #pragma unroll
     for (int i = 0; i < 16 / ROWS; ++i) {
         const int row = (i * 8 + wave) * ROWS, mine = row + lane * ROWS / 64;
-        load_to_lds(from + row * R * 2, (mine - row) * R * 2 + ((lane % (64 / ROWS)) ^ (mine & 7)) * 16, uniform(lds_address(w + row * R)));
+        load_to_lds(from + row * R * 2, (mine - row) * R * 2 + ((lane % (64 / ROWS)) ^ (mine & 15)) * 16, uniform(lds_address(w + row * R)));
     }
     wait_loads_and_meet<0>();
     const int n_waves = gridDim.x / n_heads * 8;
