@@ -81,9 +81,9 @@ __global__ __launch_bounds__(64) void absorb_kernel(const LatentShape sh, const 
 // product in the layout that the value product takes them in, and waves meet once a tile.  K and V are the same bytes; V's operand is
 // columns of a token-major page: ds_read_b64_tr_b16 reads 4 tokens x 16 columns transposed.
 // What bounds it: every wave reads the whole tile from LDS, for K and for V, 1088 KiB a tile and workgroup, which at 128 bytes a clock
-// is 8700 clocks against 4350 of products (the counters: LDS active for 0.38, matrix units for 0.40 of the time; the rest is waits of two
-// waves a SIMD for operands, the tile's meeting and the issue of the next one).  (32 rows a wave, 4 waves, would halve that, but 144 + 256 registers leave none for operands
-// in flight: it spilled.  Two groups of 4 waves in turns, one at its products while the other weighs, took 884 us where this takes 793.)
+// is 8700 clocks against 4350 of products; the matrix units are busy for 0.40 of the time.  (32 rows a wave, 4 waves, would halve that,
+// but 144 + 256 registers leave none for operands in flight: it spilled.  Two groups of 4 waves in turns, one at its products while the
+// other weighs, took 884 us where one group of 8 took 793.)
 // Bringing a tile to LDS blocks the waves that ask for it (1230 clocks for its 72 KiB from the L2, 2200 from memory), so many rows a
 // tile matter (a workgroup of 64 rows, whose waves shared the work by pages and columns, took 6300 clocks a tile), and waves without
 // rows bring the tiles of items that leave some.  At 8 requests x 16 branches over 32768 shared tokens each and 32 single sequences, 64
